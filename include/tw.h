@@ -270,6 +270,74 @@ int tw_dense_gemm(const void* A, int lda, const void* B, int ldb, void* C, int l
 int tw_dense_gemm_bias_act(const void* A, int lda, const void* B, int ldb, const void* bias, tw_act act,
                            void* C, int ldc, int M, int N, int K, tw_dtype dt, void* hip_stream);
 
+/* ---- what lies between the products of a Transformer layer (Sec. VI "Kernel Fusion": the non-GEMM operators that a sparse
+ * product's gain has to be defended against) ---- */
+
+/* Layer norm over the features of every token, row-major (a row per token):
+ *   mu = mean_n X[m,n],  rstd = 1 / sqrt(mean_n (X[m,n] - mu)^2 + eps),  Y[m,n] = (X[m,n] - mu) * rstd * gamma[n] + beta[n]
+ *   X, Y         device, M x N of type dt, ldx, ldy >= N; 2-byte aligned rows suffice, fastest with 16-byte aligned bases (gamma
+ *                and beta too) and pitches that are multiples of 8 (rows of X are then read in 16-byte pieces, i.e. up to
+ *                the next multiple of 8 columns: the buffer must hold M x ldx elements), and N <= 16384.  Y may be X (same pitch);
+ *                otherwise they must not overlap
+ *   gamma, beta  device, N elements of type dt each, or NULL for ones / zeros
+ *   eps          >= 0 and finite
+ *   mean, rstd   device, M floats each for a backward pass, or NULL
+ * Sums are fp32, the variance is taken about the mean, Y is rounded once.  Non-finite values stay within their row.
+ * M >= 0 (M = 0 enqueues nothing).  One kernel, no workspace; it can be recorded into a HIP graph.
+ * Errors: TW_ERR_ARG (null X or Y, negative M, N <= 0, pitch too small, unknown dt, eps), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED
+ * (N above 2^24 - 256; tw_layernorm_t also M above 2^28), TW_ERR_HIP. */
+int tw_layernorm(const void* X, int ldx, int M, int N, const void* gamma, const void* beta, float eps, void* Y, int ldy,
+                 float* mean, float* rstd, tw_dtype dt, void* hip_stream);
+
+/* The same on the transposed boundary: Xt and Yt are N x M (a row per feature, a column per token), ldxt, ldyt >= M; gamma and
+ * beta have an element per ROW.  Fastest with 16-byte aligned bases and pitches that are multiples of 8 (then the buffer must hold
+ * N x ldxt elements), of 64 best, and N <= 2048. */
+int tw_layernorm_t(const void* Xt, int ldxt, int M, int N, const void* gamma, const void* beta, float eps, void* Yt, int ldyt,
+                   float* mean, float* rstd, tw_dtype dt, void* hip_stream);
+
+/* Backward pass of tw_layernorm.  With xh = (X - mean) * rstd and g = dY * gamma, per row:
+ *   dX = rstd * (g - mean_n(g) - xh * mean_n(g * xh)),   dgamma[n] = sum_m dY[m,n] * xh[m,n],   dbeta[n] = sum_m dY[m,n]
+ *   dY, X, dX      device, M x N of type dt, pitches and alignment as in tw_layernorm; dX may be dY or X (same pitch), otherwise it
+ *                  must not overlap them
+ *   gamma          as in the forward pass (NULL: ones)
+ *   mean, rstd     device, M floats each, as tw_layernorm left them
+ *   dgamma, dbeta  device, N floats each, or NULL where not wanted; overwritten
+ *   workspace      device, tw_layernorm_grad_workspace bytes, 16-byte aligned, no initial value; calls that overlap in time need
+ *                  one each
+ * Sums are fp32; those over rows are added in a fixed order (no atomics), so repeated calls give the same bits.  Kernels only, so
+ * the call can be recorded into a HIP graph.  M = 0 leaves zeros in dgamma and dbeta.
+ * Errors: as tw_layernorm, and TW_ERR_BUF for a workspace that is too small. */
+int tw_layernorm_grad_workspace(int M, int N, size_t* ws_bytes);
+int tw_layernorm_grad(const void* dY, int lddy, const void* X, int ldx, int M, int N, const void* gamma, const float* mean,
+                      const float* rstd, void* dX, int lddx, float* dgamma, float* dbeta, void* workspace, size_t ws_bytes,
+                      tw_dtype dt, void* hip_stream);
+
+/* Attention over whole prompts, row-major, between the fused QKV product and the output product of a layer.  The M tokens are packed
+ * sequences of any lengths: sequence s holds the tokens [seq_start[s], seq_start[s+1]).  For token i of a sequence and head h
+ *   O[i, h] = sum_j p_ij V[j, h / (heads / kv_heads)],   p_ij = softmax over j of scale * Q[i, h] . K[j, h / (heads / kv_heads)]
+ * over the tokens j of the same sequence, with causal != 0 only those j <= i.
+ *   Q, O       device, M x (heads * head_dim) of type dt, a head's features side by side, ldq, ldo at least that; O may be Q (same
+ *              pitch), otherwise it must not overlap Q, K or V
+ *   K, V       device, M x (kv_heads * head_dim), ldk, ldv at least that.  Q, K and V may be column ranges of one matrix.  16-byte aligned
+ *              bases, pitches that are multiples of 8
+ *   seq_start  device, n_seqs + 1 ascending int32 (equal neighbours: an empty sequence), 4-byte aligned; NULL: one sequence of all
+ *              M tokens (n_seqs 0 or 1).  Tokens in front of seq_start[0] and from seq_start[n_seqs] on are no sequence's: their rows of
+ *              O are left as they were and nothing of them reaches another row.  Values outside 0 .. M count as the nearest inside;
+ *              what a list that does not ascend gives is unspecified, but nothing outside the matrices is touched.
+ *   heads      a multiple of kv_heads
+ *   head_dim   a multiple of 8, at most 128
+ *   scale      >= 0 and finite (1 / sqrt(head_dim) as a rule)
+ * Scores, softmax statistics and sums are fp32; the weights p are rounded to dt for the product with V, O is rounded once.  A token that a row
+ * does not see leaves it untouched, whatever its values; non-finite scores or values that it sees give what the formula gives
+ * (NaN, or inf where the infinities agree).
+ * M >= 0 (M = 0 enqueues nothing).  One kernel, no workspace; it can be recorded into a HIP graph (the lengths are read when it runs).
+ * Errors: TW_ERR_ARG (null pointer, negative M or n_seqs, heads not a multiple of kv_heads, pitch too small, scale, unknown dt, no
+ * seq_start and n_seqs > 1), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED (head_dim; ldk or ldv of 2^24 and more; heads * ceil(M / 128) of 2^24
+ * and more), TW_ERR_HIP. */
+int tw_attention(const void* Q, int ldq, const void* K, int ldk, const void* V, int ldv, void* O, int ldo, int M,
+                 const int* seq_start, int n_seqs, int heads, int kv_heads, int head_dim, float scale, int causal, tw_dtype dt,
+                 void* hip_stream);
+
 const char* tw_strerror(int status);
 int tw_version(void);
 

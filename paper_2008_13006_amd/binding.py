@@ -7,6 +7,7 @@ fallback of any kind.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional, Tuple
@@ -20,8 +21,8 @@ TW_F16, TW_BF16 = 0, 1
 _DT = {"f16": TW_F16, "bf16": TW_BF16}
 
 SYMBOLS = ["tw_pack_size", "tw_pack", "tw_pack_tew_size", "tw_pack_tew", "tw_restore_ew", "tw_unpack", "tw_info", "tw_prune", "tw_gemm_workspace", "tw_gemm_plan", "tw_gemm", "tw_gemm_static",
-           "tw_gemm_bias_act", "tw_gemm_t", "tw_gemm_t_bias_act", "tw_transpose", "tw_dense_gemm", "tw_dense_gemm_bias_act", "tw_strerror",
-           "tw_version"]
+           "tw_gemm_bias_act", "tw_gemm_t", "tw_gemm_t_bias_act", "tw_transpose", "tw_dense_gemm", "tw_dense_gemm_bias_act", "tw_layernorm",
+           "tw_layernorm_t", "tw_layernorm_grad_workspace", "tw_layernorm_grad", "tw_attention", "tw_strerror", "tw_version"]
 TW_ACT_NONE, TW_ACT_RELU, TW_ACT_GELU = 0, 1, 2
 TW_STATIC_SCRATCH_BYTES = 8 << 20   # include/tw.h
 _ACT = {None: TW_ACT_NONE, "none": TW_ACT_NONE, "relu": TW_ACT_RELU, "gelu": TW_ACT_GELU}
@@ -75,6 +76,11 @@ def _load() -> ctypes.CDLL:
     lib.tw_gemm_t_bias_act.argtypes = [vp, vp, vp, i, i, vp, i, vp, i, vp, sz, vp]
     lib.tw_transpose.argtypes = [vp, i, i, i, vp, i, vp]
     lib.tw_dense_gemm_bias_act.argtypes = [vp, i, vp, i, vp, i, vp, i, i, i, i, i, vp]
+    f = ctypes.c_float
+    lib.tw_layernorm.argtypes = lib.tw_layernorm_t.argtypes = [vp, i, i, i, vp, vp, f, vp, i, vp, vp, i, vp]
+    lib.tw_layernorm_grad_workspace.argtypes = [i, i, ctypes.POINTER(sz)]
+    lib.tw_layernorm_grad.argtypes = [vp, i, vp, i, i, i, vp, vp, vp, vp, i, vp, vp, vp, sz, i, vp]
+    lib.tw_attention.argtypes = [vp, i, vp, i, vp, i, vp, i, i, vp, i, i, i, i, f, i, i, vp]
     lib.tw_strerror.argtypes = [i]
     lib.tw_strerror.restype = ctypes.c_char_p
     for name in SYMBOLS:
@@ -463,6 +469,112 @@ def tw_dense_gemm(A, B, C=None, stream=None):
     _check(_lib.tw_dense_gemm(A.data_ptr(), lda, B.data_ptr(), ldb,
                               C.data_ptr(), ldc, M, N, K, dt, _stream_ptr(stream)), "tw_dense_gemm")
     return C
+
+
+def _dt_code(t) -> int:
+    torch = _torch()
+    assert t.dtype in (torch.float16, torch.bfloat16)
+    return TW_F16 if t.dtype == torch.float16 else TW_BF16
+
+
+def _matrix(t, shape, like) -> int:
+    """Checks a matrix operand (GPU, type and device of `like`, unit column stride); its pitch, which one row leaves open."""
+    assert t.is_cuda and t.dtype == like.dtype and t.device == like.device and tuple(t.shape) == tuple(shape)
+    assert shape[1] <= 1 or t.stride(1) == 1
+    return t.stride(0) if shape[0] > 1 and shape[1] > 0 else max(int(shape[1]), 1)
+
+
+def _vector(t, n, dtype, like):
+    """Checks a vector operand (n elements side by side on the device of `like`); its pointer, None for none."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.device == like.device and tuple(t.shape) == (n,) and (n <= 1 or t.stride(0) == 1)
+    return t.data_ptr()
+
+
+def _new_matrix(rows, cols, like):
+    """An output of the pitch that the kernels take 16 bytes at a time."""
+    return _torch().empty((rows, -(-cols // 8) * 8), dtype=like.dtype, device=like.device)[:, :cols]
+
+
+def _layernorm(entry, where, X, M, N, gamma, beta, eps, Y, mean, rstd, stream):
+    torch = _torch()
+    assert X.is_cuda and X.dim() == 2
+    dt = _dt_code(X)
+    if Y is None:
+        Y = _new_matrix(*X.shape, X)
+    ldx, ldy = _matrix(X, X.shape, X), _matrix(Y, X.shape, X)
+    g, b = _vector(gamma, N, X.dtype, X), _vector(beta, N, X.dtype, X)
+    mu, rs = _vector(mean, M, torch.float32, X), _vector(rstd, M, torch.float32, X)
+    _check(entry(X.data_ptr(), ldx, M, N, g, b, float(eps), Y.data_ptr(), ldy, mu, rs, dt, _stream_ptr(stream)), where)
+    return Y
+
+
+def tw_layernorm(X, gamma=None, beta=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
+    """Layer norm of every row of X [M, N]; gamma, beta: [N] of X's type or None.  mean, rstd: float32 [M] to be filled
+    for a backward pass, or None.  Y may be X."""
+    return _layernorm(_lib.tw_layernorm, "tw_layernorm", X, X.shape[0], X.shape[1], gamma, beta, eps, Y, mean, rstd, stream)
+
+
+def tw_layernorm_t(Xt, gamma=None, beta=None, eps=1e-5, Yt=None, mean=None, rstd=None, stream=None):
+    """Layer norm of every COLUMN of Xt [N, M] (the transposed boundary: a row per feature); gamma, beta: [N] or None."""
+    return _layernorm(_lib.tw_layernorm_t, "tw_layernorm_t", Xt, Xt.shape[1], Xt.shape[0], gamma, beta, eps, Yt, mean, rstd, stream)
+
+
+def tw_layernorm_grad_workspace(M: int, N: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.tw_layernorm_grad_workspace(int(M), int(N), ctypes.byref(n)), "tw_layernorm_grad_workspace")
+    return int(n.value)
+
+
+def tw_layernorm_grad(dY, X, gamma, mean, rstd, dX=None, dgamma=None, dbeta=None, workspace=None, stream=None):
+    """Backward pass of tw_layernorm: (dX, dgamma, dbeta), the sums over rows as float32 [N].  mean, rstd: what the forward pass
+    left.  dX may be dY or X.  workspace: a uint8 tensor of tw_layernorm_grad_workspace bytes, or None for one of torch's caching allocator."""
+    torch = _torch()
+    assert X.is_cuda and X.dim() == 2
+    M, N = X.shape
+    dt = _dt_code(X)
+    on = torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+    with on:                                   # (what is allocated here belongs to the stream that uses it)
+        if dX is None:
+            dX = _new_matrix(M, N, X)
+        if dgamma is None:
+            dgamma = torch.empty(N, dtype=torch.float32, device=X.device)
+        if dbeta is None:
+            dbeta = torch.empty(N, dtype=torch.float32, device=X.device)
+        if workspace is None:
+            workspace = torch.empty(tw_layernorm_grad_workspace(M, N), dtype=torch.uint8, device=X.device)
+    assert workspace.is_cuda and workspace.device == X.device and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+    lddy, ldx, lddx = (_matrix(t, (M, N), X) for t in (dY, X, dX))
+    g = _vector(gamma, N, X.dtype, X)
+    f32 = [_vector(t, n, torch.float32, X) for t, n in ((mean, M), (rstd, M), (dgamma, N), (dbeta, N))]
+    _check(_lib.tw_layernorm_grad(dY.data_ptr(), lddy, X.data_ptr(), ldx, M, N, g, f32[0], f32[1], dX.data_ptr(), lddx, f32[2], f32[3],
+                                  workspace.data_ptr(), workspace.numel(), dt, _stream_ptr(stream)), "tw_layernorm_grad")
+    return dX, dgamma, dbeta
+
+
+def tw_attention(Q, K, V, seq_start, heads: int, kv_heads: Optional[int] = None, scale: Optional[float] = None, causal=True, O=None,
+                 stream=None):
+    """Attention over packed sequences.  Q: [M, heads * d], K and V: [M, kv_heads * d] (column ranges of one matrix as a rule);
+    seq_start: int32 [n_seqs + 1] on the GPU, or None for one sequence.  kv_heads: heads by default; scale: 1 / sqrt(d) by default.  Returns
+    O [M, heads * d], whose rows outside every sequence are left as they were.  O may be Q."""
+    torch = _torch()
+    assert Q.is_cuda and Q.dim() == 2 and heads > 0 and Q.shape[1] % heads == 0
+    kv_heads = heads if kv_heads is None else kv_heads
+    M, d = Q.shape[0], Q.shape[1] // heads
+    dt = _dt_code(Q)
+    if O is None:
+        O = _new_matrix(M, heads * d, Q)
+    ldq, ldo = _matrix(Q, (M, heads * d), Q), _matrix(O, (M, heads * d), Q)
+    ldk, ldv = _matrix(K, (M, kv_heads * d), Q), _matrix(V, (M, kv_heads * d), Q)
+    n_seqs, starts = 0, None
+    if seq_start is not None:
+        assert seq_start.dim() == 1 and seq_start.numel() >= 1
+        n_seqs = seq_start.numel() - 1
+        starts = _vector(seq_start, n_seqs + 1, torch.int32, Q)
+    _check(_lib.tw_attention(Q.data_ptr(), ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, O.data_ptr(), ldo, M, starts, n_seqs, heads, kv_heads, d,
+                             d ** -0.5 if scale is None else float(scale), int(bool(causal)), dt, _stream_ptr(stream)), "tw_attention")
+    return O
 
 
 def bits_to_tensor(bits: np.ndarray, dtype: str, device="cuda:0"):

@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtw.so")
-SOURCES = ["tw_pack.cpp", "tw_gemm.hip", "tw_dense.hip"]
+SOURCES = ["tw_pack.cpp", "tw_gemm.hip", "tw_dense.hip", "tw_layernorm.hip", "tw_attention.hip"]
 HEADERS = ["tw_format.h", "tw_device.hpp", "tw_pieces.h", os.path.join("..", "..", "include", "tw.h")]
 
 
@@ -28,7 +28,8 @@ def needs_build() -> bool:
 
 # (source, -D flags, object): tw_gemm.hip is compiled as its host code (part 0) and eight groups of kernels
 # (parts 1..4: fp16 / bf16 x plain / fused epilogue; 5..8: the same with the code for TEW blobs), all at once
-UNITS = [("tw_pack.cpp", [], "tw_pack.cpp.o"), ("tw_dense.hip", [], "tw_dense.hip.o")] + [
+UNITS = [("tw_pack.cpp", [], "tw_pack.cpp.o"), ("tw_dense.hip", [], "tw_dense.hip.o"),
+         ("tw_layernorm.hip", [], "tw_layernorm.hip.o"), ("tw_attention.hip", [], "tw_attention.hip.o")] + [
     ("tw_gemm.hip", [f"-DTW_PART={i}"], f"tw_gemm.part{i}.o") for i in range(9)]
 
 

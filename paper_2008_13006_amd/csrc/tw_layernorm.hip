@@ -1,0 +1,657 @@
+// Layer norm between the products of a network (Sec. VI "Kernel Fusion" counts Add-bias + LayerNorm among what eats a sparse
+// product's gain; the addition rides in the product's epilogue, this is the rest).
+//
+//   mu = mean_n x[n],  rstd = 1 / sqrt(mean_n (x[n] - mu)^2 + eps),  y[n] = (x[n] - mu) rstd gamma[n] + beta[n]
+//   backward, with xh = (x - mu) rstd and g = dy gamma:
+//     dx = rstd (g - mean_n g - xh mean_n(g xh)),   dgamma[n] = sum_m dy xh,   dbeta[n] = sum_m dy
+//
+// All of it is bound by memory: forward 4 bytes an element, backward 6.  A row is read once and waits in registers for its
+// statistics (the variance is taken about the mean, not as a difference of two large sums); everything is fp32, rounded once at the store.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "../../include/tw.h"
+#include "tw_device.hpp"
+
+namespace {
+
+typedef unsigned short us;
+
+struct LnParams {
+    const us* x;
+    const us* gamma;            // null: ones
+    const us* beta;             // null: zeros
+    us* y;
+    float* mean;                // null: not wanted
+    float* rstd;
+    long ldx, ldy;
+    int M, N;
+    float eps;
+};
+
+// Sum over groups of TPR consecutive lanes, the same bits in every lane of the group.
+template <int TPR>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int s = 1; s < TPR && s < 64; s <<= 1) v += __shfl_xor(v, s);
+    return v;
+}
+
+template <int DT>
+__device__ __forceinline__ void unpack8(tw_u32x4 v, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = tw_to_f32<DT>((us)(v[i] & 0xFFFFu));
+        f[2 * i + 1] = tw_to_f32<DT>((us)(v[i] >> 16));
+    }
+}
+template <int DT>
+__device__ __forceinline__ tw_u32x4 pack8(const float (&f)[8]) {
+    tw_u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (unsigned)tw_cvt<DT>(f[2 * i]) | ((unsigned)tw_cvt<DT>(f[2 * i + 1]) << 16);
+    return v;
+}
+// Eight parameters from index c on; those from N on are zero and not read.
+template <int DT, bool TAIL>
+__device__ __forceinline__ void params8(const us* src, int c, int N, float (&f)[8]) {
+    if (!TAIL || c + 8 <= N) {
+        unpack8<DT>(*(const tw_u32x4*)(src + c), f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = c + e < N ? tw_to_f32<DT>(src[c + e]) : 0.f;
+    }
+}
+template <bool TAIL>
+__device__ __forceinline__ void put8(us* dst, int left, tw_u32x4 v) {   // left: elements up to the row's end
+    if (!TAIL || left >= 8) {
+        *(tw_u32x4*)dst = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < left) dst[e] = (us)(v[e >> 1] >> (16 * (e & 1)));
+    }
+}
+
+// Sum over the TPR threads of a row: lanes of a wave, or the four waves of a workgroup (`red`: two rows of four floats, used in turn).
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float (&red)[2][4], int turn) {
+    v = group_sum<TPR>(v);
+    if constexpr (TPR == 256) {
+        if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = (red[turn][0] + red[turn][1]) + (red[turn][2] + red[turn][3]);
+    }
+    return v;
+}
+
+// Row-major, 16-byte pieces.  TPR threads of a workgroup of 256 share a row, thread t of them the pieces t, t + TPR, .. (PER of
+// them); TAIL: N is no multiple of 8, the last piece reaches into the row's pitch.
+template <int DT, int TPR, int PER, bool TAIL>
+__global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
+    constexpr int kGroups = 256 / TPR;
+    __shared__ float red[2][4];
+    const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+    const float inv_n = 1.f / (float)p.N;
+    for (long m0 = (long)blockIdx.x * kGroups; m0 < p.M; m0 += (long)gridDim.x * kGroups) {   // (uniform: the barriers are met by all)
+        const long m = m0 + grp < p.M ? m0 + grp : p.M - 1;   // (groups behind the last row repeat it and store nothing)
+        const bool mine = m0 + grp < p.M;
+        const us* row = p.x + m * p.ldx;
+        float v[PER][8];
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = 8 * (t + i * TPR);
+            tw_u32x4 w{0u, 0u, 0u, 0u};
+            if (c < p.N) w = *(const tw_u32x4*)(row + c);
+            unpack8<DT>(w, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = 8 * (t + i * TPR);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (TAIL && c + e >= p.N) v[i][e] = 0.f;
+                s += v[i][e];
+            }
+        }
+        const float mean = row_sum<TPR>(s, red, 0) * inv_n;
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = 8 * (t + i * TPR);
+            if (c < p.N) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[i][e] -= mean;
+                    if (!TAIL || c + e < p.N) q = __builtin_fmaf(v[i][e], v[i][e], q);
+                }
+            }
+        }
+        const float rstd = 1.f / sqrtf(row_sum<TPR>(q, red, 1) * inv_n + p.eps);
+        if (mine && t == 0) {
+            if (p.mean) p.mean[m] = mean;
+            if (p.rstd) p.rstd[m] = rstd;
+        }
+        us* out = p.y + m * p.ldy;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = 8 * (t + i * TPR);
+            if (c < p.N && mine) {
+                float g[8], b[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] = 1.f, b[e] = 0.f;
+                if (p.gamma) params8<DT, TAIL>(p.gamma, c, p.N, g);
+                if (p.beta) params8<DT, TAIL>(p.beta, c, p.N, b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf(v[i][e] * rstd, g[e], b[e]);
+                put8<TAIL>(out + c, p.N - c, pack8<DT>(v[i]));
+            }
+        }
+    }
+}
+
+// Row-major, any pitch, any alignment, any N: a workgroup per row reads it three times, element by element (from the caches after the
+// first).
+template <int DT>
+__global__ __launch_bounds__(256) void tw_ln_any_kernel(const LnParams p) {
+    __shared__ float red[2][4];
+    const float inv_n = 1.f / (float)p.N;
+    for (long m = blockIdx.x; m < p.M; m += gridDim.x) {
+        const us* row = p.x + m * p.ldx;
+        float s = 0.f;
+        for (int c = threadIdx.x; c < p.N; c += 256) s += tw_to_f32<DT>(row[c]);
+        const float mean = row_sum<256>(s, red, 0) * inv_n;
+        float q = 0.f;
+        for (int c = threadIdx.x; c < p.N; c += 256) {
+            const float d = tw_to_f32<DT>(row[c]) - mean;
+            q = __builtin_fmaf(d, d, q);
+        }
+        const float rstd = 1.f / sqrtf(row_sum<256>(q, red, 1) * inv_n + p.eps);
+        if (threadIdx.x == 0) {
+            if (p.mean) p.mean[m] = mean;
+            if (p.rstd) p.rstd[m] = rstd;
+        }
+        us* out = p.y + m * p.ldy;
+        for (int c = threadIdx.x; c < p.N; c += 256) {
+            const float g = p.gamma ? tw_to_f32<DT>(p.gamma[c]) : 1.f, b = p.beta ? tw_to_f32<DT>(p.beta[c]) : 0.f;
+            out[c] = tw_cvt<DT>(__builtin_fmaf((tw_to_f32<DT>(row[c]) - mean) * rstd, g, b));
+        }
+    }
+}
+
+// The same pieces, as ones the compiler knows nothing of: it then unpacks them again where they are used, and does not keep the
+// unpacked values (eight registers a piece instead of four) from one phase to the next.
+template <int PER>
+__device__ __forceinline__ void forget(tw_u32x4 (&w)[PER]) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) asm volatile("" : "+v"(w[i]));
+}
+
+// Transposed boundary: features are rows, tokens columns.  A workgroup takes 64 tokens (a line of every row), a lane the 16-byte piece
+// lane % 8 of row lane / 8 + 8 * wave + 8 * WAVES * i, PER of them, which wait in registers as they were read.  A token's sums meet across
+// the eight lanes of a wave that hold its piece and, through LDS, across the waves.
+template <int DT, int WAVES, int PER>
+__global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
+    constexpr int kRows = 8 * WAVES;
+    __shared__ float red[2][WAVES][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pc = lane & 7;
+    const long m0 = (long)blockIdx.x * 64 + 8 * pc;
+    const int n0 = 8 * wave + (lane >> 3);
+    const bool here = m0 < p.M;
+    const float inv_n = 1.f / (float)p.N;
+    tw_u32x4 w[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        w[i] = tw_u32x4{0u, 0u, 0u, 0u};
+        if (here && n0 + kRows * i < p.N) w[i] = tw_load16_stream(p.x + (long)(n0 + kRows * i) * p.ldx + m0);
+    }
+    auto across = [&](float (&s)[8], int turn) {             // sums of the eight tokens over all rows
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[e] += __shfl_xor(s[e], 8);
+            s[e] += __shfl_xor(s[e], 16);
+            s[e] += __shfl_xor(s[e], 32);
+        }
+        if (lane < 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) red[turn][wave][8 * pc + e] = s[e];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) s[e] += red[turn][k][8 * pc + e];
+        }
+    };
+    float mean[8] = {}, rstd[8] = {};
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        float f[8];
+        unpack8<DT>(w[i], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mean[e] += f[e];
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    across(mean, 0);
+    forget(w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mean[e] *= inv_n;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        float f[8];
+        unpack8<DT>(w[i], f);
+        if (n0 + kRows * i < p.N) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = f[e] - mean[e];
+                rstd[e] = __builtin_fmaf(d, d, rstd[e]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    across(rstd, 1);
+    forget(w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rstd[e] = 1.f / sqrtf(rstd[e] * inv_n + p.eps);
+    if (!here) return;
+    if (threadIdx.x < 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (m0 + e < p.M) {
+                if (p.mean) p.mean[m0 + e] = mean[e];
+                if (p.rstd) p.rstd[m0 + e] = rstd[e];
+            }
+    }
+    const int left = p.M - m0 < 8 ? (int)(p.M - m0) : 8;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int n = n0 + kRows * i;
+        if (n >= p.N) continue;
+        const float g = p.gamma ? tw_to_f32<DT>(p.gamma[n]) : 1.f, b = p.beta ? tw_to_f32<DT>(p.beta[n]) : 0.f;
+        float f[8];
+        unpack8<DT>(w[i], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf((f[e] - mean[e]) * rstd[e], g, b);
+        put8<true>(p.y + (long)n * p.ldy + m0, left, pack8<DT>(f));
+    }
+}
+
+// Transposed boundary, any pitch, alignment and N: a lane per token, the rows dealt out to the waves, read three times.
+template <int DT>
+__global__ __launch_bounds__(1024) void tw_ln_t_any_kernel(const LnParams p) {
+    __shared__ float red[2][16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long m = (long)blockIdx.x * 64 + lane;
+    const long mc = m < p.M ? m : p.M - 1;
+    const float inv_n = 1.f / (float)p.N;
+    auto across = [&](float s, int turn) {
+        red[turn][wave][lane] = s;
+        __syncthreads();
+        s = 0.f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s += red[turn][k][lane];
+        return s;
+    };
+    float s = 0.f;
+    for (int n = wave; n < p.N; n += 16) s += tw_to_f32<DT>(p.x[(long)n * p.ldx + mc]);
+    const float mean = across(s, 0) * inv_n;
+    s = 0.f;
+    for (int n = wave; n < p.N; n += 16) {
+        const float d = tw_to_f32<DT>(p.x[(long)n * p.ldx + mc]) - mean;
+        s = __builtin_fmaf(d, d, s);
+    }
+    const float rstd = 1.f / sqrtf(across(s, 1) * inv_n + p.eps);
+    if (m >= p.M) return;
+    if (wave == 0) {
+        if (p.mean) p.mean[m] = mean;
+        if (p.rstd) p.rstd[m] = rstd;
+    }
+    for (int n = wave; n < p.N; n += 16) {
+        const float g = p.gamma ? tw_to_f32<DT>(p.gamma[n]) : 1.f, b = p.beta ? tw_to_f32<DT>(p.beta[n]) : 0.f;
+        p.y[(long)n * p.ldy + m] = tw_cvt<DT>(__builtin_fmaf((tw_to_f32<DT>(p.x[(long)n * p.ldx + m]) - mean) * rstd, g, b));
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ backward
+struct LnGradParams {
+    const us* dy;
+    const us* x;
+    const us* gamma;
+    const float* mean;
+    const float* rstd;
+    us* dx;
+    float* part_gamma;          // [n_parts][N]: a workgroup's sums over its rows
+    float* part_beta;
+    float* row_stats;           // tw_ln_grad_rows_kernel: [M][2]: mean g, mean g xh
+    long lddy, ldx, lddx;
+    int M, N, rows_per_part;
+};
+
+// Row-major, 16-byte pieces, threads and pieces as tw_ln_kernel.  A workgroup walks its rows; a thread's share of dgamma and
+// dbeta stays in registers all the way, the shares of the workgroup's row groups meet in LDS at the end, and the
+// workgroups' sums are added by a second kernel in a fixed order (no atomics: repeated calls give the same bits).
+template <int DT, int TPR, int PER, bool TAIL>
+__global__ __launch_bounds__(256) void tw_ln_grad_kernel(const LnGradParams p) {
+    constexpr int kGroups = 256 / TPR;
+    __shared__ float red[2][4];
+    extern __shared__ __attribute__((aligned(16))) float share[];            // [kGroups][TPR * PER * 8]
+    const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+    const float inv_n = 1.f / (float)p.N;
+    const long first = (long)blockIdx.x * p.rows_per_part;
+    const long last = first + p.rows_per_part < p.M ? first + p.rows_per_part : p.M;
+    float sg[PER][8], sb[PER][8];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sg[i][e] = sb[i][e] = 0.f;
+    for (long m0 = first; m0 < last; m0 += kGroups) {
+        const bool mine = m0 + grp < last;
+        const long m = mine ? m0 + grp : last - 1;
+        const float mean = p.mean[m], rstd = p.rstd[m];
+        tw_u32x4 wx[PER], wd[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = 8 * (t + i * TPR);
+            wx[i] = wd[i] = tw_u32x4{0u, 0u, 0u, 0u};
+            if (c < p.N) {
+                wx[i] = *(const tw_u32x4*)(p.x + m * p.ldx + c);
+                wd[i] = *(const tw_u32x4*)(p.dy + m * p.lddy + c);
+            }
+        }
+        float c1 = 0.f, c2 = 0.f;
+        float xh[PER][8], g[PER][8];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = 8 * (t + i * TPR);
+            if (c < p.N) {
+                float f[8], d[8], ga[8];
+                unpack8<DT>(wx[i], f);
+                unpack8<DT>(wd[i], d);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ga[e] = 1.f;
+                if (p.gamma) params8<DT, TAIL>(p.gamma, c, p.N, ga);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (TAIL && c + e >= p.N) f[e] = mean, d[e] = 0.f;
+                    xh[i][e] = (f[e] - mean) * rstd;
+                    g[i][e] = d[e] * ga[e];
+                    if (mine) {
+                        sg[i][e] = __builtin_fmaf(d[e], xh[i][e], sg[i][e]);
+                        sb[i][e] += d[e];
+                    }
+                    c1 += g[i][e];
+                    c2 = __builtin_fmaf(g[i][e], xh[i][e], c2);
+                }
+            }
+        }
+        if constexpr (TPR == 256) {
+            c1 = group_sum<64>(c1);
+            c2 = group_sum<64>(c2);
+            __syncthreads();                                 // everyone is through with the last row's sums
+            if ((threadIdx.x & 63) == 0) {
+                red[0][threadIdx.x >> 6] = c1;
+                red[1][threadIdx.x >> 6] = c2;
+            }
+            __syncthreads();
+            c1 = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
+            c2 = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+        } else {
+            c1 = group_sum<TPR>(c1);
+            c2 = group_sum<TPR>(c2);
+        }
+        c1 *= inv_n;
+        c2 *= inv_n;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = 8 * (t + i * TPR);
+            if (c < p.N && mine) {
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = rstd * (g[i][e] - c1 - xh[i][e] * c2);
+                put8<TAIL>(p.dx + m * p.lddx + c, p.N - c, pack8<DT>(o));
+            }
+        }
+    }
+    if constexpr (TPR == 256) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = 8 * (t + i * TPR) + e;
+                if (c < p.N) {
+                    p.part_gamma[(long)blockIdx.x * p.N + c] = sg[i][e];
+                    p.part_beta[(long)blockIdx.x * p.N + c] = sb[i][e];
+                }
+            }
+    } else {
+        constexpr int kCols = TPR * PER * 8;
+        auto meet = [&](const float (&s)[PER][8], float* out) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) share[grp * kCols + 8 * (t + i * TPR) + e] = s[i][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < p.N; c += 256) {
+                float v = 0.f;
+#pragma unroll
+                for (int k = 0; k < kGroups; ++k) v += share[k * kCols + c];
+                out[(long)blockIdx.x * p.N + c] = v;
+            }
+        };
+        meet(sg, p.part_gamma);
+        meet(sb, p.part_beta);
+    }
+}
+
+// Any pitch, alignment and N, two kernels: the rows' two means, then a thread per column that walks a run of rows.
+template <int DT>
+__global__ __launch_bounds__(256) void tw_ln_grad_rows_kernel(const LnGradParams p) {
+    __shared__ float red[2][4];
+    const float inv_n = 1.f / (float)p.N;
+    for (long m = blockIdx.x; m < p.M; m += gridDim.x) {
+        const float mean = p.mean[m], rstd = p.rstd[m];
+        float c1 = 0.f, c2 = 0.f;
+        for (int c = threadIdx.x; c < p.N; c += 256) {
+            const float g = tw_to_f32<DT>(p.dy[m * p.lddy + c]) * (p.gamma ? tw_to_f32<DT>(p.gamma[c]) : 1.f);
+            c1 += g;
+            c2 = __builtin_fmaf(g, (tw_to_f32<DT>(p.x[m * p.ldx + c]) - mean) * rstd, c2);
+        }
+        c1 = row_sum<256>(c1, red, 0);
+        c2 = row_sum<256>(c2, red, 1);
+        if (threadIdx.x == 0) {
+            p.row_stats[2 * m] = c1 * inv_n;
+            p.row_stats[2 * m + 1] = c2 * inv_n;
+        }
+    }
+}
+template <int DT>
+__global__ __launch_bounds__(256) void tw_ln_grad_cols_kernel(const LnGradParams p) {
+    const long c = (long)blockIdx.y * 256 + threadIdx.x;
+    if (c >= p.N) return;
+    const long first = (long)blockIdx.x * p.rows_per_part;
+    const long last = first + p.rows_per_part < p.M ? first + p.rows_per_part : p.M;
+    const float ga = p.gamma ? tw_to_f32<DT>(p.gamma[c]) : 1.f;
+    float sg = 0.f, sb = 0.f;
+    for (long m = first; m < last; ++m) {
+        const float d = tw_to_f32<DT>(p.dy[m * p.lddy + c]), rstd = p.rstd[m];
+        const float xh = (tw_to_f32<DT>(p.x[m * p.ldx + c]) - p.mean[m]) * rstd;
+        sg = __builtin_fmaf(d, xh, sg);
+        sb += d;
+        p.dx[m * p.lddx + c] = tw_cvt<DT>(rstd * (d * ga - p.row_stats[2 * m] - xh * p.row_stats[2 * m + 1]));
+    }
+    p.part_gamma[(long)blockIdx.x * p.N + c] = sg;
+    p.part_beta[(long)blockIdx.x * p.N + c] = sb;
+}
+
+// dst[n] = sum over the parts, 64 columns to a workgroup, every fourth part to a wave, then the four waves' sums in order.
+// blockIdx.y: dgamma or dbeta.
+__global__ __launch_bounds__(256) void tw_ln_grad_sum_kernel(const float* part_gamma, const float* part_beta, int n_parts, int N,
+                                                             float* dgamma, float* dbeta) {
+    __shared__ float red[4][64];
+    const float* src = blockIdx.y ? part_beta : part_gamma;
+    float* dst = blockIdx.y ? dbeta : dgamma;
+    if (!dst) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long c = (long)blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (c < N)
+        for (int k = wave; k < n_parts; k += 4) s += src[(long)k * N + c];
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < N) dst[c] = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+constexpr int kMaxFeatures = (1 << 24) - 256;   // (the grids of the backward pass' column kernels)
+
+// Threads of a row and 16-byte pieces of a thread for N features; false: the row does not fit the registers of 256 threads.
+bool row_shape(int N, int& tpr, int& per) {
+    const int pieces = (N - 1) / 8 + 1;
+    if (pieces <= 16) { tpr = 16; per = 1; }
+    else if (pieces <= 32) { tpr = 32; per = 1; }
+    else if (pieces <= 256) { tpr = 64; per = (pieces + 63) / 64; }
+    else if (pieces <= 512) { tpr = 256; per = 2; }
+    else if (pieces <= 1024) { tpr = 256; per = 4; }
+    else if (pieces <= 2048) { tpr = 256; per = 8; }
+    else return false;
+    return true;
+}
+
+template <template <int, int, int, bool> class K, int DT, bool TAIL>
+const void* pick_shape(int tpr, int per) {
+    if (tpr == 16) return K<DT, 16, 1, TAIL>::fn();
+    if (tpr == 32) return K<DT, 32, 1, TAIL>::fn();
+    if (tpr == 64) return per == 1 ? K<DT, 64, 1, TAIL>::fn() : per == 2 ? K<DT, 64, 2, TAIL>::fn() : per == 3 ? K<DT, 64, 3, TAIL>::fn() : K<DT, 64, 4, TAIL>::fn();
+    return per == 2 ? K<DT, 256, 2, TAIL>::fn() : per == 4 ? K<DT, 256, 4, TAIL>::fn() : K<DT, 256, 8, TAIL>::fn();
+}
+template <template <int, int, int, bool> class K>
+const void* pick(tw_dtype dt, int tpr, int per, bool tail) {
+    if (dt == TW_F16) return tail ? pick_shape<K, TW_F16, true>(tpr, per) : pick_shape<K, TW_F16, false>(tpr, per);
+    return tail ? pick_shape<K, TW_BF16, true>(tpr, per) : pick_shape<K, TW_BF16, false>(tpr, per);
+}
+template <int DT, int TPR, int PER, bool TAIL> struct Forward {
+    static const void* fn() { return (const void*)tw_ln_kernel<DT, TPR, PER, TAIL>; }
+};
+template <int DT, int TPR, int PER, bool TAIL> struct Backward {
+    static const void* fn() { return (const void*)tw_ln_grad_kernel<DT, TPR, PER, TAIL>; }
+};
+
+template <int DT>
+const void* pick_t(int N) {
+    if (N <= 256) return (const void*)tw_ln_t_kernel<DT, 8, 4>;
+    if (N <= 512) return (const void*)tw_ln_t_kernel<DT, 8, 8>;
+    if (N <= 768) return (const void*)tw_ln_t_kernel<DT, 8, 12>;
+    return N <= 1024 ? (const void*)tw_ln_t_kernel<DT, 8, 16> : (const void*)tw_ln_t_kernel<DT, 16, 16>;
+}
+
+bool odd(const void* q) { return ((uintptr_t)q & 1) != 0; }
+bool vec16(const void* q) { return ((uintptr_t)q & 15) == 0; }
+
+int check_forward(const void* X, int ldx, int M, int N, const void* gamma, const void* beta, float eps, const void* Y, int ldy,
+                  const float* mean, const float* rstd, tw_dtype dt, int inner) {
+    if ((M > 0 && (!X || !Y)) || M < 0 || N <= 0 || ldx < inner || ldy < inner) return TW_ERR_ARG;
+    if (dt != TW_F16 && dt != TW_BF16) return TW_ERR_ARG;
+    if (!(eps >= 0.f) || std::isinf(eps)) return TW_ERR_ARG;
+    if (N > kMaxFeatures) return TW_ERR_UNSUPPORTED;
+    if (odd(X) || odd(Y) || odd(gamma) || odd(beta) || ((uintptr_t)mean & 3) != 0 || ((uintptr_t)rstd & 3) != 0) return TW_ERR_ALIGN;
+    return TW_OK;
+}
+// Grids in the first dimension are capped (the kernels over rows walk on): a launch holds fewer than 2^32 threads there.
+unsigned capped(long blocks) { return (unsigned)(blocks < (1L << 22) ? blocks : (1L << 22)); }
+
+int launch(const void* fn, dim3 grid, dim3 block, void* params, size_t lds, void* stream) {
+    void* args[] = {params};
+    return hipLaunchKernel(fn, grid, block, args, lds, (hipStream_t)stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
+}
+
+// Workgroups of the backward pass: each leaves N sums of dgamma and of dbeta.
+int grad_parts(int M) {
+    const int want = (M + 15) / 16;
+    return want < 512 ? want : 512;
+}
+}  // namespace
+
+extern "C" int tw_layernorm(const void* X, int ldx, int M, int N, const void* gamma, const void* beta, float eps, void* Y, int ldy,
+                            float* mean, float* rstd, tw_dtype dt, void* hip_stream) {
+    const int rc = check_forward(X, ldx, M, N, gamma, beta, eps, Y, ldy, mean, rstd, dt, N);
+    if (rc) return rc;
+    if (M == 0) return TW_OK;
+    LnParams p{(const us*)X, (const us*)gamma, (const us*)beta, (us*)Y, mean, rstd, ldx, ldy, M, N, eps};
+    int tpr = 0, per = 0;
+    const bool vec = vec16(X) && vec16(Y) && vec16(gamma) && vec16(beta) && (ldx & 7) == 0 && (ldy & 7) == 0;
+    if (vec && row_shape(N, tpr, per)) {
+        const long groups = 256 / tpr, blocks = (M + groups - 1) / groups;
+        return launch(pick<Forward>(dt, tpr, per, (N & 7) != 0), dim3(capped(blocks)), dim3(256), &p, 0, hip_stream);
+    }
+    const void* fn = dt == TW_F16 ? (const void*)tw_ln_any_kernel<TW_F16> : (const void*)tw_ln_any_kernel<TW_BF16>;
+    return launch(fn, dim3(capped(M)), dim3(256), &p, 0, hip_stream);
+}
+
+extern "C" int tw_layernorm_t(const void* Xt, int ldxt, int M, int N, const void* gamma, const void* beta, float eps, void* Yt, int ldyt,
+                              float* mean, float* rstd, tw_dtype dt, void* hip_stream) {
+    const int rc = check_forward(Xt, ldxt, M, N, gamma, beta, eps, Yt, ldyt, mean, rstd, dt, M);
+    if (rc) return rc;
+    if (M == 0) return TW_OK;
+    LnParams p{(const us*)Xt, (const us*)gamma, (const us*)beta, (us*)Yt, mean, rstd, ldxt, ldyt, M, N, eps};
+    if (M > (1 << 28)) return TW_ERR_UNSUPPORTED;            // (a workgroup of up to 1024 threads per 64 tokens)
+    const dim3 grid((unsigned)((M + 63L) / 64));
+    const bool vec = vec16(Xt) && vec16(Yt) && (ldxt & 7) == 0 && (ldyt & 7) == 0;
+    if (vec && N <= 2048)
+        return launch(dt == TW_F16 ? pick_t<TW_F16>(N) : pick_t<TW_BF16>(N), grid, dim3(N <= 1024 ? 512 : 1024), &p, 0, hip_stream);
+    const void* fn = dt == TW_F16 ? (const void*)tw_ln_t_any_kernel<TW_F16> : (const void*)tw_ln_t_any_kernel<TW_BF16>;
+    return launch(fn, grid, dim3(1024), &p, 0, hip_stream);
+}
+
+extern "C" int tw_layernorm_grad_workspace(int M, int N, size_t* ws_bytes) {
+    if (!ws_bytes || M < 0 || N <= 0) return TW_ERR_ARG;
+    *ws_bytes = 4 * ((size_t)grad_parts(M) * 2 * (size_t)N + 2 * (size_t)M);
+    return TW_OK;
+}
+
+extern "C" int tw_layernorm_grad(const void* dY, int lddy, const void* X, int ldx, int M, int N, const void* gamma, const float* mean,
+                                 const float* rstd, void* dX, int lddx, float* dgamma, float* dbeta, void* workspace, size_t ws_bytes,
+                                 tw_dtype dt, void* hip_stream) {
+    if ((M > 0 && (!dY || !X || !mean || !rstd || !dX || !workspace)) || M < 0 || N <= 0) return TW_ERR_ARG;
+    if (dt != TW_F16 && dt != TW_BF16) return TW_ERR_ARG;
+    if (lddy < N || ldx < N || lddx < N) return TW_ERR_ARG;
+    if (N > kMaxFeatures) return TW_ERR_UNSUPPORTED;
+    if (odd(dY) || odd(X) || odd(dX) || odd(gamma)) return TW_ERR_ALIGN;
+    if ((((uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)dgamma | (uintptr_t)dbeta) & 3) != 0 || !vec16(workspace)) return TW_ERR_ALIGN;
+    size_t need = 0;
+    tw_layernorm_grad_workspace(M, N, &need);
+    if (ws_bytes < need) return TW_ERR_BUF;
+    const int parts = grad_parts(M);
+    LnGradParams p;
+    p.dy = (const us*)dY; p.x = (const us*)X; p.gamma = (const us*)gamma; p.mean = mean; p.rstd = rstd; p.dx = (us*)dX;
+    p.part_gamma = (float*)workspace; p.part_beta = p.part_gamma + (size_t)parts * N; p.row_stats = p.part_beta + (size_t)parts * N;
+    p.lddy = lddy; p.ldx = ldx; p.lddx = lddx; p.M = M; p.N = N;
+    p.rows_per_part = parts > 0 ? (M + parts - 1) / parts : 0;
+    int rc = TW_OK;
+    if (M > 0) {
+        int tpr = 0, per = 0;
+        const bool vec = vec16(dY) && vec16(X) && vec16(dX) && vec16(gamma) && ((lddy | ldx | lddx) & 7) == 0;
+        if (vec && row_shape(N, tpr, per)) {
+            const size_t lds = tpr == 256 ? 0 : (size_t)256 * per * 8 * 4;
+            rc = launch(pick<Backward>(dt, tpr, per, (N & 7) != 0), dim3((unsigned)parts), dim3(256), &p, lds, hip_stream);
+        } else {
+            const unsigned gy = (unsigned)((N + 255) / 256);
+            rc = launch(dt == TW_F16 ? (const void*)tw_ln_grad_rows_kernel<TW_F16> : (const void*)tw_ln_grad_rows_kernel<TW_BF16>,
+                        dim3(capped(M)), dim3(256), &p, 0, hip_stream);
+            if (!rc)
+                rc = launch(dt == TW_F16 ? (const void*)tw_ln_grad_cols_kernel<TW_F16> : (const void*)tw_ln_grad_cols_kernel<TW_BF16>,
+                            dim3((unsigned)parts, gy), dim3(256), &p, 0, hip_stream);
+        }
+        if (rc) return rc;
+    }
+    if (!dgamma && !dbeta) return TW_OK;
+    int n_parts = parts, n = N;                              // (M = 0: no part, the sums are zero)
+    const float* pg = p.part_gamma;
+    const float* pb = p.part_beta;
+    void* args[] = {(void*)&pg, (void*)&pb, (void*)&n_parts, (void*)&n, (void*)&dgamma, (void*)&dbeta};
+    return hipLaunchKernel((const void*)tw_ln_grad_sum_kernel, dim3((unsigned)(((long)N + 63) / 64), 2), dim3(256), args, 0,
+                           (hipStream_t)hip_stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
+}

@@ -1,0 +1,71 @@
+"""What the entry points between the products refuse, and what they take without a GPU call: no GPU needed, nothing is launched."""
+import ctypes
+
+import pytest
+
+from paper_2008_13006_amd import binding as tw
+
+ARG, BUF, ALIGN, UNSUPPORTED = -1, -3, -4, -6
+P = 0x10000          # stands for a device pointer: checked, never read (every call below ends before a launch)
+
+
+def ln(entry="tw_layernorm", X=P, ld=64, M=4, N=64, gamma=P, beta=P, eps=1e-5, Y=P, ldy=64, mean=None, rstd=None, dt=0):
+    return getattr(tw._lib, entry)(X, ld, M, N, gamma, beta, eps, Y, ldy, mean, rstd, dt, None)
+
+
+@pytest.mark.parametrize("entry", ["tw_layernorm", "tw_layernorm_t"])
+def test_layernorm_refusals(entry):
+    wide = dict(M=64, N=4) if entry == "tw_layernorm_t" else {}
+    bad = [(dict(X=None), ARG), (dict(Y=None), ARG), (dict(M=-1), ARG), (dict(N=0), ARG), (dict(N=-3), ARG), (dict(ld=63), ARG), (dict(ldy=63), ARG),
+           (dict(dt=2), ARG), (dict(dt=-1), ARG), (dict(eps=-1e-9), ARG), (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG),
+           (dict(X=P + 1), ALIGN), (dict(Y=P + 1), ALIGN), (dict(gamma=P + 1), ALIGN), (dict(beta=P + 1), ALIGN), (dict(mean=P + 2), ALIGN),
+           (dict(rstd=P + 1), ALIGN)]
+    for kw, want in bad:
+        if entry == "tw_layernorm_t" and "N" not in kw:
+            kw = {**wide, **kw}
+        assert ln(entry, **kw) == want, kw
+    assert ln(entry, N=1 << 24, ld=1 << 24, ldy=1 << 24) == UNSUPPORTED
+    assert ln(entry, M=0, X=None, Y=None) == 0
+    if entry == "tw_layernorm_t":
+        assert ln(entry, M=(1 << 28) + 1, N=1, ld=1 << 29, ldy=1 << 29) == UNSUPPORTED
+
+
+def grad(dY=P, lddy=64, X=P, ldx=64, M=4, N=64, gamma=P, mean=P, rstd=P, dX=P, lddx=64, dgamma=None, dbeta=None, ws=P, nbytes=None, dt=0):
+    if nbytes is None:
+        nbytes = tw.tw_layernorm_grad_workspace(max(M, 0), max(N, 1))
+    return tw._lib.tw_layernorm_grad(dY, lddy, X, ldx, M, N, gamma, mean, rstd, dX, lddx, dgamma, dbeta, ws, nbytes, dt, None)
+
+
+def test_layernorm_grad_refusals():
+    for kw, want in [(dict(dY=None), ARG), (dict(X=None), ARG), (dict(mean=None), ARG), (dict(rstd=None), ARG), (dict(dX=None), ARG), (dict(ws=None), ARG),
+                     (dict(M=-1), ARG), (dict(N=0), ARG), (dict(dt=7), ARG), (dict(lddy=63), ARG), (dict(ldx=63), ARG), (dict(lddx=63), ARG),
+                     (dict(dY=P + 1), ALIGN), (dict(X=P + 1), ALIGN), (dict(dX=P + 1), ALIGN), (dict(gamma=P + 1), ALIGN), (dict(mean=P + 2), ALIGN),
+                     (dict(rstd=P + 2), ALIGN), (dict(dgamma=P + 2), ALIGN), (dict(dbeta=P + 1), ALIGN), (dict(ws=P + 8), ALIGN),
+                     (dict(nbytes=tw.tw_layernorm_grad_workspace(4, 64) - 1), BUF),
+                     (dict(N=1 << 24, lddy=1 << 24, ldx=1 << 24, lddx=1 << 24), UNSUPPORTED)]:
+        assert grad(**kw) == want, kw
+    assert grad(M=0, dY=None, X=None, mean=None, rstd=None, dX=None, ws=None, nbytes=0) == 0   # (no sums wanted: nothing to do)
+    n = ctypes.c_size_t(0)
+    for args, want in [((-1, 4), ARG), ((4, 0), ARG)]:
+        assert tw._lib.tw_layernorm_grad_workspace(*args, ctypes.byref(n)) == want
+    assert tw._lib.tw_layernorm_grad_workspace(4, 4, None) == ARG
+    # room for the sums of at most 512 groups of rows and two numbers a row
+    assert tw.tw_layernorm_grad_workspace(1, 5) == 4 * (2 * 5 + 2) and tw.tw_layernorm_grad_workspace(10 ** 6, 768) == 4 * (1024 * 768 + 2 * 10 ** 6)
+
+
+def attention(Q=P, ldq=128, K=P, ldk=64, V=P, ldv=64, O=P, ldo=128, M=4, seq_start=P, n_seqs=1, heads=2, kv_heads=1, d=64, scale=0.125, causal=1, dt=0):
+    return tw._lib.tw_attention(Q, ldq, K, ldk, V, ldv, O, ldo, M, seq_start, n_seqs, heads, kv_heads, d, scale, causal, dt, None)
+
+
+def test_attention_refusals():
+    for kw, want in [(dict(Q=None), ARG), (dict(K=None), ARG), (dict(V=None), ARG), (dict(O=None), ARG), (dict(M=-1), ARG), (dict(n_seqs=-1), ARG),
+                     (dict(heads=0), ARG), (dict(kv_heads=0), ARG), (dict(heads=3, kv_heads=2, ldq=192, ldo=192, ldk=128, ldv=128), ARG), (dict(d=0), ARG),
+                     (dict(dt=2), ARG), (dict(scale=-1.0), ARG), (dict(scale=float("nan")), ARG), (dict(scale=float("inf")), ARG),
+                     (dict(seq_start=None, n_seqs=2), ARG), (dict(ldq=120), ARG), (dict(ldk=56), ARG), (dict(ldv=56), ARG), (dict(ldo=120), ARG),
+                     (dict(d=136, ldq=272, ldk=136, ldv=136, ldo=272), UNSUPPORTED), (dict(d=60), UNSUPPORTED), (dict(ldq=130), ALIGN), (dict(ldk=68), ALIGN),
+                     (dict(ldv=68), ALIGN), (dict(ldo=132), ALIGN), (dict(Q=P + 8), ALIGN), (dict(K=P + 2), ALIGN), (dict(V=P + 4), ALIGN),
+                     (dict(O=P + 8), ALIGN), (dict(seq_start=P + 2), ALIGN), (dict(ldk=1 << 24), UNSUPPORTED), (dict(ldv=1 << 24), UNSUPPORTED),
+                     (dict(M=1 << 30), UNSUPPORTED)]:
+        assert attention(**kw) == want, kw
+    assert attention(M=0, Q=None, K=None, V=None, O=None) == 0
+    assert attention(n_seqs=0) == 0                              # no sequence, no row
