@@ -254,6 +254,25 @@ int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, const void* 
                        const void* bias, tw_act act, void* Ct, int ldct, void* workspace, size_t ws_bytes,
                        void* hip_stream);
 
+/* C = act(A . (B * mask) + bias) + R: tw_gemm_bias_act with the addition that follows the second product of either half of a Transformer
+ * layer (the residual connection) in its epilogue.
+ *   R    device, M x N elements of the blob's dtype, ldr >= N; 2-byte aligned rows suffice.  R may be C (same pitch: the product is
+ *        added to C; not for a TEW blob with residual weights in pruned columns); otherwise the two must not overlap
+ *   bias, act  as in tw_gemm_bias_act (NULL and TW_ACT_NONE: the plain product plus R)
+ * The sum of the fp32 result and R is rounded once to the storage type.  A pruned column n of C holds act(bias[n]) + R[m, n].
+ * Everything else as tw_gemm_bias_act; TW_ERR_ARG also for a null R, ldr < N, R = C with another pitch; TW_ERR_UNSUPPORTED also for
+ * ldr >= 2^23 and for R = C where a TEW blob rules it out. */
+int tw_gemm_bias_act_add(const void* blob_host, const void* blob_dev, const void* A, int M, int lda,
+                         const void* bias, tw_act act, const void* R, int ldr, void* C, int ldc, void* workspace,
+                         size_t ws_bytes, void* hip_stream);
+
+/* Ct = (act(A . (B * mask) + bias))^T + Rt, the same on the transposed boundary.  Rt: N x M row-major as Ct, ldrt >= M, ldrt % 8 == 0,
+ * 16-byte aligned; rows are read in 16-byte pieces up to the pitch (which may be any multiple of 8).  Rt may be Ct under the same
+ * conditions. */
+int tw_gemm_t_bias_act_add(const void* blob_host, const void* blob_dev, const void* At, int M, int ldat,
+                           const void* bias, tw_act act, const void* Rt, int ldrt, void* Ct, int ldct, void* workspace,
+                           size_t ws_bytes, void* hip_stream);
+
 /* dst[c, r] = src[r, c] for a rows x cols matrix of 16-bit elements (device pointers, row-major, ld in
  * elements): the transposes at the two ends of a network whose layers run on the transposed boundary
  * (Sec. VI "Kernel Fusion" counts them, unfused, at about 10 % of the latency). */
@@ -269,6 +288,11 @@ int tw_dense_gemm(const void* A, int lda, const void* B, int ldb, void* C, int l
 /* C = act(A . B + bias), the dense yardstick with the same fused epilogue (bias: N elements of dt). */
 int tw_dense_gemm_bias_act(const void* A, int lda, const void* B, int ldb, const void* bias, tw_act act,
                            void* C, int ldc, int M, int N, int K, tw_dtype dt, void* hip_stream);
+
+/* C = act(A . B + bias) + R, the dense yardstick with the same addition (R: M x N, ldr >= N, ldr % 8 == 0, 16-byte aligned; R may be C
+ * with the same pitch, otherwise they must not overlap; nothing is read behind its last element). */
+int tw_dense_gemm_bias_act_add(const void* A, int lda, const void* B, int ldb, const void* bias, tw_act act, const void* R, int ldr,
+                               void* C, int ldc, int M, int N, int K, tw_dtype dt, void* hip_stream);
 
 /* ---- what lies between the products of a Transformer layer (Sec. VI "Kernel Fusion": the non-GEMM operators that a sparse
  * product's gain has to be defended against) ---- */

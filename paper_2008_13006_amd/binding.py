@@ -21,7 +21,8 @@ TW_F16, TW_BF16 = 0, 1
 _DT = {"f16": TW_F16, "bf16": TW_BF16}
 
 SYMBOLS = ["tw_pack_size", "tw_pack", "tw_pack_tew_size", "tw_pack_tew", "tw_restore_ew", "tw_unpack", "tw_info", "tw_prune", "tw_gemm_workspace", "tw_gemm_plan", "tw_gemm", "tw_gemm_static",
-           "tw_gemm_bias_act", "tw_gemm_t", "tw_gemm_t_bias_act", "tw_transpose", "tw_dense_gemm", "tw_dense_gemm_bias_act", "tw_layernorm",
+           "tw_gemm_bias_act", "tw_gemm_t", "tw_gemm_t_bias_act", "tw_transpose", "tw_dense_gemm", "tw_dense_gemm_bias_act", "tw_gemm_bias_act_add",
+           "tw_gemm_t_bias_act_add", "tw_dense_gemm_bias_act_add", "tw_layernorm",
            "tw_layernorm_t", "tw_layernorm_grad_workspace", "tw_layernorm_grad", "tw_attention", "tw_strerror", "tw_version"]
 TW_ACT_NONE, TW_ACT_RELU, TW_ACT_GELU = 0, 1, 2
 TW_STATIC_SCRATCH_BYTES = 8 << 20   # include/tw.h
@@ -77,6 +78,8 @@ def _load() -> ctypes.CDLL:
     lib.tw_transpose.argtypes = [vp, i, i, i, vp, i, vp]
     lib.tw_dense_gemm_bias_act.argtypes = [vp, i, vp, i, vp, i, vp, i, i, i, i, i, vp]
     f = ctypes.c_float
+    lib.tw_gemm_bias_act_add.argtypes = lib.tw_gemm_t_bias_act_add.argtypes = [vp, vp, vp, i, i, vp, i, vp, i, vp, i, vp, sz, vp]
+    lib.tw_dense_gemm_bias_act_add.argtypes = [vp, i, vp, i, vp, i, vp, i, vp, i, i, i, i, i, vp]
     lib.tw_layernorm.argtypes = lib.tw_layernorm_t.argtypes = [vp, i, i, i, vp, vp, f, vp, i, vp, vp, i, vp]
     lib.tw_layernorm_grad_workspace.argtypes = [i, i, ctypes.POINTER(sz)]
     lib.tw_layernorm_grad.argtypes = [vp, i, vp, i, i, i, vp, vp, vp, vp, i, vp, vp, vp, sz, i, vp]
@@ -484,6 +487,12 @@ def _matrix(t, shape, like) -> int:
     return t.stride(0) if shape[0] > 1 and shape[1] > 0 else max(int(shape[1]), 1)
 
 
+def _matrix8(t, shape, like) -> int:
+    """The same for entry points whose pitches are multiples of 8: a single row's may be any."""
+    ld = _matrix(t, shape, like)
+    return ld if shape[0] > 1 else -(-ld // 8) * 8
+
+
 def _vector(t, n, dtype, like):
     """Checks a vector operand (n elements side by side on the device of `like`); its pointer, None for none."""
     if t is None:
@@ -495,6 +504,52 @@ def _vector(t, n, dtype, like):
 def _new_matrix(rows, cols, like):
     """An output of the pitch that the kernels take 16 bytes at a time."""
     return _torch().empty((rows, -(-cols // 8) * 8), dtype=like.dtype, device=like.device)[:, :cols]
+
+
+def tw_gemm_bias_act_add(w: TwWeight, A, R, bias=None, act="none", C=None, stream=None):
+    """C = act(A . (B * mask) + bias) + R.  R: torch tensor [M, N] of A's type; C may be R (see include/tw.h)."""
+    M, N = _row_operands(w, A, C)
+    if C is None:
+        C = _torch().empty((M, N), dtype=A.dtype, device=A.device)
+    ldr = _matrix(R, (M, N), A)
+    b = _vector(bias, N, A.dtype, A)
+    lda, ldc = A.stride(0), C.stride(0)
+    if M <= 1:
+        lda, ldc = max(w.info["K"], lda), N
+    ws, ws_bytes = w.workspace_for(M)
+    _check(_lib.tw_gemm_bias_act_add(w._blob_ptr, w.blob_dev.data_ptr(), A.data_ptr(), M, lda, b, _act_code(act), R.data_ptr(), ldr,
+                                     C.data_ptr(), ldc, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm_bias_act_add")
+    return C
+
+
+def tw_gemm_t_bias_act_add(w: TwWeight, At, Rt, bias=None, act="none", Ct=None, stream=None):
+    """Ct = act(A . (B * mask) + bias)^T + Rt from At = A^T.  Rt: torch tensor [N, M]; Ct may be Rt (see include/tw.h)."""
+    assert At.is_cuda and At.dtype == w.torch_dtype and At.dim() == 2 and At.shape[0] == w.info["K"]
+    K, M = At.shape
+    N = w.info["N"]
+    if Ct is None:
+        Ct = _torch().empty((N, (M + 63) // 64 * 64), dtype=At.dtype, device=At.device)[:, :M]
+    ldat, ldrt, ldct = _matrix8(At, (K, M), At), _matrix8(Rt, (N, M), At), _matrix8(Ct, (N, M), At)
+    b = _vector(bias, N, At.dtype, At)
+    ws, ws_bytes = w.workspace_for(M)
+    _check(_lib.tw_gemm_t_bias_act_add(w._blob_ptr, w.blob_dev.data_ptr(), At.data_ptr(), M, ldat, b, _act_code(act), Rt.data_ptr(), ldrt,
+                                       Ct.data_ptr(), ldct, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm_t_bias_act_add")
+    return Ct
+
+
+def tw_dense_gemm_bias_act_add(A, B, R, bias=None, act="none", C=None, stream=None):
+    """C = act(A . B + bias) + R, all row-major torch tensors on the GPU; C may be R."""
+    assert A.is_cuda and A.dim() == 2 and B.dim() == 2
+    dt = _dt_code(A)
+    M, K = A.shape
+    N = B.shape[1]
+    if C is None:
+        C = _new_matrix(M, N, A)
+    lda, ldb, ldr, ldc = _matrix8(A, (M, K), A), _matrix8(B, (K, N), A), _matrix8(R, (M, N), A), _matrix8(C, (M, N), A)
+    b = _vector(bias, N, A.dtype, A)
+    _check(_lib.tw_dense_gemm_bias_act_add(A.data_ptr(), lda, B.data_ptr(), ldb, b, _act_code(act), R.data_ptr(), ldr, C.data_ptr(), ldc,
+                                           M, N, K, dt, _stream_ptr(stream)), "tw_dense_gemm_bias_act_add")
+    return C
 
 
 def _layernorm(entry, where, X, M, N, gamma, beta, eps, Y, mean, rstd, stream):

@@ -26,11 +26,12 @@ def needs_build() -> bool:
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
 
 
-# (source, -D flags, object): tw_gemm.hip is compiled as its host code (part 0) and eight groups of kernels
-# (parts 1..4: fp16 / bf16 x plain / fused epilogue; 5..8: the same with the code for TEW blobs), all at once
+# (source, -D flags, object): tw_gemm.hip is compiled as its host code (part 0) and twelve groups of kernels
+# (parts 1..4: fp16 / bf16 x plain / fused epilogue; 5..8: the same with the code for TEW blobs; 9, 10 and 11, 12: fp16 / bf16 with
+# an epilogue that adds a matrix, without and with that code), all at once
 UNITS = [("tw_pack.cpp", [], "tw_pack.cpp.o"), ("tw_dense.hip", [], "tw_dense.hip.o"),
          ("tw_layernorm.hip", [], "tw_layernorm.hip.o"), ("tw_attention.hip", [], "tw_attention.hip.o")] + [
-    ("tw_gemm.hip", [f"-DTW_PART={i}"], f"tw_gemm.part{i}.o") for i in range(9)]
+    ("tw_gemm.hip", [f"-DTW_PART={i}"], f"tw_gemm.part{i}.o") for i in range(13)]
 
 
 def build(force: bool = True, verbose: bool = False) -> str:

@@ -56,6 +56,8 @@ struct DenseParams {
     int nbm, nbn;
     const unsigned short* bias;   // N values added before the activation, or null
     int act;                      // tw_act
+    const unsigned short* res;    // ADD: the matrix that is added behind the activation, laid out as C with the pitch ldr
+    long ldr;
     int stream;                   // rows of C start on 128-byte boundaries: whole lines go out as streaming stores
 };
 
@@ -137,6 +139,50 @@ __device__ __forceinline__ void add_bias_act(tw_f32x16 (&acc)[2], const tw_u32x2
     }
 }
 
+// ADD: what is added to a 32 x 64 block.  It is read as the results are written (8 lanes cover the 64 columns of a row, 8 rows a request), so
+// that the requests are whole lines, and handed round through the wave's staging area in the results' own arrangement (see store_block).
+__device__ __forceinline__ void request_add(const DenseParams& p, int row0, int col0, int width, int lane, tw_u32x4 (&v)[4]) {
+    const int j = lane & 7, rows = p.M - row0 - (lane >> 3);
+    const unsigned short* src = p.res + (long)(row0 + (lane >> 3)) * p.ldr + col0 + 8 * j;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        v[q] = tw_u32x4{0u, 0u, 0u, 0u};
+        if (8 * q >= rows) continue;
+        const unsigned short* at = src + (long)(8 * q) * p.ldr;
+        if (8 * j + 8 <= width) v[q] = *(const tw_u32x4*)at;
+        else if (8 * j < width) {                              // the row's ragged end
+            unsigned e[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (8 * j + i < width) e[i >> 1] |= (unsigned)at[i] << (16 * (i & 1));
+            v[q] = tw_u32x4{e[0], e[1], e[2], e[3]};
+        }
+    }
+}
+template <int DT>
+__device__ __forceinline__ void add_block(tw_f32x16 (&acc)[2], const tw_u32x4 (&v)[4], unsigned char* stage, int lane) {
+    const int mrow = lane & 31, h = lane >> 5, j = lane & 7;
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = (lane >> 3) + 8 * q;
+        *(tw_u32x4*)(stage + r * 128 + ((j ^ ((r >> 1) & 7)) << 4)) = q >= 2 ? tw_u32x4{v[q].z, v[q].w, v[q].x, v[q].y} : v[q];
+    }
+    asm volatile("" ::: "memory");
+    const unsigned char* myrow = stage + mrow * 128 + (h ^ (mrow >> 4)) * 8;
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const tw_u32x2 a = *(const tw_u32x2*)(myrow + (((4 * cb + q) ^ ((mrow >> 1) & 7)) << 4));
+            acc[cb][4 * q] += tw_to_f32<DT>((unsigned short)(a.x & 0xFFFFu));
+            acc[cb][4 * q + 1] += tw_to_f32<DT>((unsigned short)(a.x >> 16));
+            acc[cb][4 * q + 2] += tw_to_f32<DT>((unsigned short)(a.y & 0xFFFFu));
+            acc[cb][4 * q + 3] += tw_to_f32<DT>((unsigned short)(a.y >> 16));
+        }
+    asm volatile("" ::: "memory");
+}
+
 // Writes one 32 x 64 block of a wave's results to C[row0 .., col0 .. col0 + width) through the wave's staging area of
 // 32 rows x 128 bytes.  Column octet c of row r lies at slot c ^ (r/2 % 8) of the row, its two halves swapped in
 // rows 16..31: the 8-byte writes of 32 lanes (32 rows, one octet) and the 16-byte reads (8 rows, 8 octets) then both
@@ -192,7 +238,8 @@ __device__ __forceinline__ void store_block(const tw_f32x16 (&acc)[2], unsigned 
 
 // NTA: the activations are read by one column of blocks only (N <= 256), so they carry the streaming hint.
 // WIDE: row pitches for which a block's offsets do not fit a buffer descriptor (64-bit addresses per lane instead).
-template <int DT, int MSW, bool NTA, bool WIDE>
+// ADD: the variant that adds a matrix behind the activation.
+template <int DT, int MSW, bool NTA, bool WIDE, bool ADD>
 __global__ __launch_bounds__(kThreads) void tw_dense_kernel(const DenseParams p) {
     constexpr int BM = bm_of<MSW>(), A_BYTES = a_bytes_of<MSW>(), BUF_BYTES = buf_bytes_of<MSW>(), NST = stages_of<MSW>();
     constexpr int kLoads = MSW + 4;               // requests of a wave per K step
@@ -381,9 +428,16 @@ __global__ __launch_bounds__(kThreads) void tw_dense_kernel(const DenseParams p)
             if (width > 0) {
                 tw_u32x2 bias[2][4];
                 if (fused) spread_bias(own_bias, stage, elane, bias);
+                const int row0 = m0 + wm * 32 * MSW;
+                tw_u32x4 radd[4];
+                if constexpr (ADD) request_add(p, row0, col0, width, elane, radd);
 #pragma unroll
                 for (int ms = 0; ms < MSW; ++ms) {
                     if (fused) add_bias_act<DT>(acc[ms], bias, p.act);
+                    if constexpr (ADD) {
+                        add_block<DT>(acc[ms], radd, stage, elane);
+                        if (ms + 1 < MSW) request_add(p, row0 + 32 * (ms + 1), col0, width, elane, radd);
+                    }
                     store_block<DT>(acc[ms], stage, p.C, p.ldc, m0 + wm * 32 * MSW + ms * 32, p.M, col0, width, elane, p.stream != 0);
                 }
             }
@@ -400,22 +454,20 @@ __global__ __launch_bounds__(kThreads) void tw_dense_kernel(const DenseParams p)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
+template <int DT, int MSW, bool ADD>
+const void* pick_of(bool nta, bool wide) {
+    if (wide) return (const void*)tw_dense_kernel<DT, MSW, false, true, ADD>;
+    return nta ? (const void*)tw_dense_kernel<DT, MSW, true, false, ADD> : (const void*)tw_dense_kernel<DT, MSW, false, false, ADD>;
+}
 template <int MSW>
-const void* pick(tw_dtype dt, bool nta, bool wide) {
-    if (wide) return dt == TW_F16 ? (const void*)tw_dense_kernel<TW_F16, MSW, false, true> : (const void*)tw_dense_kernel<TW_BF16, MSW, false, true>;
-    if (dt == TW_F16) return nta ? (const void*)tw_dense_kernel<TW_F16, MSW, true, false> : (const void*)tw_dense_kernel<TW_F16, MSW, false, false>;
-    return nta ? (const void*)tw_dense_kernel<TW_BF16, MSW, true, false> : (const void*)tw_dense_kernel<TW_BF16, MSW, false, false>;
+const void* pick(tw_dtype dt, bool nta, bool wide, bool add) {
+    if (add) return dt == TW_F16 ? pick_of<TW_F16, MSW, true>(nta, wide) : pick_of<TW_BF16, MSW, true>(nta, wide);
+    return dt == TW_F16 ? pick_of<TW_F16, MSW, false>(nta, wide) : pick_of<TW_BF16, MSW, false>(nta, wide);
 }
 
-}  // namespace
-
-extern "C" int tw_dense_gemm(const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K,
-                             tw_dtype dt, void* hip_stream) {
-    return tw_dense_gemm_bias_act(A, lda, B, ldb, nullptr, TW_ACT_NONE, C, ldc, M, N, K, dt, hip_stream);
-}
-
-extern "C" int tw_dense_gemm_bias_act(const void* A, int lda, const void* B, int ldb, const void* bias, tw_act act,
-                                      void* C, int ldc, int M, int N, int K, tw_dtype dt, void* hip_stream) {
+// tw_dense_gemm_bias_act and, with a matrix to add (R), tw_dense_gemm_bias_act_add
+int run_dense(const void* A, int lda, const void* B, int ldb, const void* bias, tw_act act, const void* R, int ldr, void* C, int ldc, int M,
+              int N, int K, tw_dtype dt, void* hip_stream) {
     if (!A || !B || !C || M < 0 || N <= 0 || K <= 0) return TW_ERR_ARG;
     if (act != TW_ACT_NONE && act != TW_ACT_RELU && act != TW_ACT_GELU) return TW_ERR_ARG;
     if (((uintptr_t)bias & 1) != 0) return TW_ERR_ALIGN;
@@ -429,6 +481,7 @@ extern "C" int tw_dense_gemm_bias_act(const void* A, int lda, const void* B, int
     p.lda = lda; p.ldb = ldb; p.ldc = ldc;
     p.M = M; p.N = N; p.K = K;
     p.bias = (const unsigned short*)bias; p.act = (int)act;
+    p.res = (const unsigned short*)R; p.ldr = ldr;
     p.stream = ((uintptr_t)C & 127) == 0 && (ldc & 63) == 0;
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return TW_ERR_HIP;
@@ -458,11 +511,11 @@ extern "C" int tw_dense_gemm_bias_act(const void* A, int lda, const void* B, int
     // offsets of a block (256 rows of A, 64 of B) must fit 31 bits for the kernels that address through a descriptor
     const bool wide = 256L * lda >= (1L << 30) || 64L * ldb >= (1L << 30);
     const bool nta = p.nbn == 1 && !wide;
-    if (msw == 4) { fn = pick<4>(dt, nta, wide); lds = lds_bytes_of<4>(); }
-    else if (msw == 2) { fn = pick<2>(dt, nta, wide); lds = lds_bytes_of<2>(); }
-    else { fn = pick<1>(dt, nta, wide); lds = lds_bytes_of<1>(); }
-    static std::atomic<unsigned char> lds_set[64][2][15];
-    const int slot = 3 * msw + (wide ? 2 : nta ? 1 : 0);
+    if (msw == 4) { fn = pick<4>(dt, nta, wide, R != nullptr); lds = lds_bytes_of<4>(); }
+    else if (msw == 2) { fn = pick<2>(dt, nta, wide, R != nullptr); lds = lds_bytes_of<2>(); }
+    else { fn = pick<1>(dt, nta, wide, R != nullptr); lds = lds_bytes_of<1>(); }
+    static std::atomic<unsigned char> lds_set[64][2][30];
+    const int slot = 3 * msw + (wide ? 2 : nta ? 1 : 0) + (R != nullptr ? 15 : 0);
     if (!lds_set[dev][dt][slot].load(std::memory_order_acquire)) {
         if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return TW_ERR_HIP;
         lds_set[dev][dt][slot].store(1, std::memory_order_release);
@@ -470,4 +523,22 @@ extern "C" int tw_dense_gemm_bias_act(const void* A, int lda, const void* B, int
     void* args[] = {(void*)&p};
     return hipLaunchKernel(fn, dim3((unsigned)(blocks < n_cu ? blocks : n_cu)), dim3(kThreads), args, lds, (hipStream_t)hip_stream) == hipSuccess
                ? TW_OK : TW_ERR_HIP;
+}
+}  // namespace
+
+extern "C" int tw_dense_gemm(const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K,
+                             tw_dtype dt, void* hip_stream) {
+    return tw_dense_gemm_bias_act(A, lda, B, ldb, nullptr, TW_ACT_NONE, C, ldc, M, N, K, dt, hip_stream);
+}
+
+extern "C" int tw_dense_gemm_bias_act(const void* A, int lda, const void* B, int ldb, const void* bias, tw_act act,
+                                      void* C, int ldc, int M, int N, int K, tw_dtype dt, void* hip_stream) {
+    return run_dense(A, lda, B, ldb, bias, act, nullptr, 0, C, ldc, M, N, K, dt, hip_stream);
+}
+
+extern "C" int tw_dense_gemm_bias_act_add(const void* A, int lda, const void* B, int ldb, const void* bias, tw_act act, const void* R, int ldr,
+                                          void* C, int ldc, int M, int N, int K, tw_dtype dt, void* hip_stream) {
+    if (!R || ldr < N || (R == C && ldr != ldc)) return TW_ERR_ARG;
+    if ((ldr & 7) != 0 || ((uintptr_t)R & 15) != 0) return TW_ERR_ALIGN;
+    return run_dense(A, lda, B, ldb, bias, act, R, ldr, C, ldc, M, N, K, dt, hip_stream);
 }

@@ -42,6 +42,12 @@ constexpr int prefetch_depth() { return NCB <= 2 ? 6 : 3; }
 constexpr int kIdxAhead = 6;  // steps the K indices are requested ahead (they feed the LDS gather, which itself
                               // runs one step ahead of the MFMAs)
 
+// The variants of a kernel by its epilogue (template parameter FUSED): none, bias and activation, bias and activation and the addition of
+// a matrix (a layer's residual).  Each carries only the code and registers of its own.
+constexpr int kPlain = 0, kFused = 1, kAdd = 2;
+// kAdd, row-major: an offset out of its descriptor's range; a block's own stay below 2^30 (pitches from 2^23 elements are refused)
+constexpr unsigned kAddRange = 0x7F000000u;
+
 typedef short tw_i16x4 __attribute__((ext_vector_type(4)));
 typedef float tw_f32x4 __attribute__((ext_vector_type(4)));
 
@@ -52,6 +58,8 @@ struct TwGemmParams {
     int* counters;              // [0] next item, [1] finished workgroups
     const unsigned short* bias; // fused epilogue: N values of the storage type, or null
     int act;                    // fused epilogue: tw_act
+    const unsigned short* res;  // kAdd: the matrix that is added behind the activation, laid out as C with the pitch ldr
+    long ldr;
     long lda, ldc;
     int M, K, N, T;
     int k_chunk, n_chunks, G;
@@ -534,7 +542,7 @@ __device__ __forceinline__ void apply_bias_act4(tw_f32x4 (&v)[NV], const float (
 // FUSED: the kernel variant with the fused epilogue (a bias and / or an activation); the plain variant
 // carries none of its code.  PART: a wave that stores a part of the tile; bias and activation have been applied (pruned
 // columns inside the span still take theirs here).
-template <int DT, int MS, int NCB, bool FUSED, bool PART = false, int WL = kWinLines>
+template <int DT, int MS, int NCB, int FUSED, bool PART = false, int WL = kWinLines>
 __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d, tw_f32x16 (&acc)[MS][NCB],
                                            unsigned char* stage, const unsigned (&dpos)[NCB], int row0, int lane_in,
                                            unsigned short* xbuf = nullptr,
@@ -556,6 +564,67 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
         if constexpr (!PART) apply_bias_act<MS, NCB>(acc, eb, p.act);
     }
     const int h = lane >> 5, n = lane & 31;
+    // kAdd: what is added to a pass, as its results lie in the registers (a lane's column, four rows), asked for two passes ahead: 2-byte
+    // requests, whose lanes share 64-byte pieces of a row.  (Rounding first and adding where whole rows are stored would
+    // be cheaper and round twice.)  Offsets count from the block's first row and the 8-aligned column at or below the span start; those of
+    // rows behind the block's last one and of lanes without a column are out of the descriptor's range and fetch zeros.
+    // The pruned columns of the span hold act(bias) + what is added, which differs from row to row: every pass puts its eight rows of
+    // them into the staging window.  Lane l takes column l / 8 (and l / 8 + 8, ..) of the packer's list, row l % 8.
+    constexpr int kFillAhead = 2;                            // groups of eight columns whose values are asked for ahead
+    tw_u16x4 radd[2][NCB];
+    unsigned short zadd[2][kFillAhead];
+    unsigned roff[NCB], zoff[kFillAhead];
+    float zbase[kFillAhead];
+    int zcol[kFillAhead], z0 = 0, z1 = 0;
+    const int origin = d.span_start & ~7;
+    const unsigned ldr2 = 2u * (unsigned)p.ldr;
+    __amdgpu_buffer_rsrc_t rsrc;
+    auto fill_column = [&](int g, int& col, float& base) {   // this lane's column of group g (-1: none), and act(bias) of it
+        const int at = z0 + 8 * g + (lane >> 3);
+        col = -1;
+        base = 0.f;
+        if (at < z1 && (xbuf == nullptr || ((const signed char*)(p.blob + p.off_zero_xc))[at] < 0)) {
+            col = ((const int*)(p.blob + p.off_zero_cols))[at];
+            base = tw_activate(p.bias != nullptr ? tw_to_f32<DT>(p.bias[col]) : 0.f, p.act);
+        }
+    };
+    auto fill_offset = [&](int col) { return col >= 0 ? 2u * (unsigned)(col - origin) + (unsigned)(lane & 7) * ldr2 : kAddRange; };
+    auto add_value = [&](unsigned off) { return (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rsrc, (int)off, 0, 0); };
+    auto request_add = [&](int P) {
+        if constexpr (FUSED == kAdd) {
+            // (a value the compiler cannot compute ahead: it would keep the offsets of all passes in registers)
+            const unsigned first = (unsigned)fresh((int)((unsigned)(8 * P) * ldr2));
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) radd[P & 1][cb][i] = add_value(roff[cb] + first + (unsigned)i * ldr2);
+#pragma unroll
+            for (int g = 0; g < kFillAhead; ++g) {
+                zadd[P & 1][g] = 0;
+                if (8 * g < z1 - z0) zadd[P & 1][g] = add_value(zoff[g] + first);   // wave-uniform condition
+            }
+        }
+    };
+    auto added = [&](float x, int P, int cb, int i) {
+        if constexpr (FUSED == kAdd) return x + tw_to_f32<DT>(radd[P & 1][cb][i]);
+        else return x;
+    };
+    if constexpr (FUSED == kAdd) {
+        const int rows = block_end(p, row0) - row0;
+        rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(p.res + (long)row0 * p.ldr + origin), 0,
+                                                 (int)((unsigned)(rows - 1) * ldr2 + 2u * (unsigned)(p.N - origin)), 0x00020000);
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb) roff[cb] = dpos[cb] != 0xFFFFFFFFu ? 2u * dpos[cb] + (unsigned)(4 * h) * ldr2 : kAddRange;
+        if (d.span_w != d.w) {                               // wave-uniform
+            z0 = fetch_int((const int*)(p.blob + p.off_zero_ptr), d.tile);
+            z1 = fetch_int((const int*)(p.blob + p.off_zero_ptr), d.tile + 1);
+        }
+#pragma unroll
+        for (int g = 0; g < kFillAhead; ++g) {
+            fill_column(g, zcol[g], zbase[g]);
+            zoff[g] = fill_offset(zcol[g]);
+        }
+    }
     const int blk = lane >> 4, j = lane & 15;
     // read-back, as the lane that supplies an address: column offset e, group g -> (piece, row quad)
     const int in_piece = 2 * blk + (j & 1), in_rq = (j >> 1) & 1, in_e = j >> 2;
@@ -621,9 +690,25 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
 #pragma unroll
             for (int cb = 0; cb < NCB; ++cb) {
                 tw_u32x2 v;
-                v.x = (unsigned)tw_cvt<DT>(acc[ms][cb][4 * q + 0]) | ((unsigned)tw_cvt<DT>(acc[ms][cb][4 * q + 1]) << 16);
-                v.y = (unsigned)tw_cvt<DT>(acc[ms][cb][4 * q + 2]) | ((unsigned)tw_cvt<DT>(acc[ms][cb][4 * q + 3]) << 16);
+                v.x = (unsigned)tw_cvt<DT>(added(acc[ms][cb][4 * q + 0], P, cb, 0)) | ((unsigned)tw_cvt<DT>(added(acc[ms][cb][4 * q + 1], P, cb, 1)) << 16);
+                v.y = (unsigned)tw_cvt<DT>(added(acc[ms][cb][4 * q + 2], P, cb, 2)) | ((unsigned)tw_cvt<DT>(added(acc[ms][cb][4 * q + 3], P, cb, 3)) << 16);
                 *(tw_u32x2*)wpos[cb] = v;
+            }
+            if constexpr (FUSED == kAdd) {
+                auto put = [&](int col, float x) {
+                    const unsigned rel = (unsigned)(col - win0);
+                    if (col >= 0 && rel < (unsigned)kCols)
+                        *(unsigned short*)(stage + ((lane >> 2) & 1) * kPlane + rel * 8u + (lane & 3) * 2) = tw_cvt<DT>(x);
+                };
+#pragma unroll
+                for (int g = 0; g < kFillAhead; ++g)
+                    if (8 * g < z1 - z0) put(zcol[g], zbase[g] + tw_to_f32<DT>(zadd[P & 1][g]));      // wave-uniform conditions
+                for (int g = kFillAhead; 8 * g < z1 - z0; ++g) {
+                    int col;
+                    float base;
+                    fill_column(g, col, base);
+                    put(col, base + tw_to_f32<DT>(add_value(fill_offset(col) + (unsigned)(8 * P) * ldr2)));
+                }
             }
             if (nx > 0) {                                    // wave-uniform
 #pragma unroll
@@ -636,7 +721,7 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
         // clear both planes once: the passes all write the same columns.  With a fused epilogue a pruned
         // column holds act(bias) in every row instead of zero.
         tw_compiler_fence();
-        if (!fused || d.span_w == d.w) {
+        if (!fused || FUSED == kAdd || d.span_w == d.w) {
 #pragma unroll
             for (int pl = 0; pl < 2; ++pl)
 #pragma unroll
@@ -657,7 +742,11 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
         tw_compiler_fence();
 #pragma unroll
         for (int P = 0; P < NP; ++P)
-            if (P == pass0) write_pass(P);
+            if (P == pass0) {
+                request_add(P);
+                if (P + 1 < NP && P + 1 < pass1) request_add(P + 1);
+                write_pass(P);
+            }
         tw_compiler_fence();
 #pragma unroll
         for (int P = 0; P < NP; ++P) {
@@ -671,6 +760,7 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
             const unsigned short eF = *(const unsigned short*)ragF;
             const unsigned short eL = *(const unsigned short*)ragL;
             tw_compiler_fence();
+            if (P + 2 < NP && P + 2 < pass1) request_add(P + 2);
             if (P + 1 < NP && P + 1 < pass1) write_pass(P + 1);
             tw_compiler_fence();
 #pragma unroll
@@ -689,7 +779,8 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
             }
             // At most a few of this wave's stores stay in flight: a long queue of stores in the CU's memory
             // pipeline holds up the loads of the waves that are multiplying (no load of this wave is pending here).
-            asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+            // (kAdd: the waits for what is added see to that; this one would wait for what has been asked for ahead.)
+            if constexpr (FUSED != kAdd) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
         }
         tw_compiler_fence();
     }
@@ -863,7 +954,7 @@ __device__ __forceinline__ void stage_commit(const TwGemmParams& p, const ARegs<
 // The destination row of a staged row comes from the lane that owns that packed column
 // (ds_bpermute).  The pruned columns inside the tile's span are written as lines of zeros from the
 // packer's list.
-template <int DT, int MS, int NCB, bool FUSED, bool PART = false>
+template <int DT, int MS, int NCB, int FUSED, bool PART = false>
 __device__ __forceinline__ void store_tile_t(const TwGemmParams& p, const TileU& d, tw_f32x16 (&acc)[MS][NCB],
                                              unsigned char* stage, const unsigned (&dpos)[NCB], int m0, int lane_in,
                                              int cb0 = 0, int cb1 = NCB, const unsigned short* xbuf = nullptr,
@@ -900,10 +991,52 @@ __device__ __forceinline__ void store_tile_t(const TwGemmParams& p, const TileU&
                 if (8 * pc + e < mleft) dst[e] = (unsigned short)(w[e >> 1] >> (16 * (e & 1)));
         }
     };
+    // kAdd: the rows that are added, read like the results are written (whole rows of the block), handed round through the same staging
+    // area, and the next column block's on their way while this one's are added.  A piece is read up to the row's pitch.
+    auto get_piece = [&](long row) {
+        tw_u32x4 v{0u, 0u, 0u, 0u};
+        if (8 * pc < mleft) v = *(const tw_u32x4*)(p.res + row * p.ldr + (m0 + 8 * pc));
+        return v;
+    };
+    tw_u32x4 radd[32 / RPI];
+    auto request_add = [&](int cb) {
+        if constexpr (FUSED == kAdd) {
+#pragma unroll
+            for (int i = 0; i < 32 / RPI; ++i) {
+                const unsigned dcol = (unsigned)__builtin_amdgcn_ds_bpermute((rr + RPI * i) * 4, (int)dpos[cb]);
+                radd[i] = tw_u32x4{0u, 0u, 0u, 0u};
+                if (dcol != 0xFFFFFFFFu) radd[i] = get_piece((long)origin + (long)dcol);
+            }
+        }
+    };
+#pragma unroll
+    for (int cb = 0; cb < NCB; ++cb)
+        if (cb == cb0) request_add(cb);
 #pragma unroll
     for (int cb = 0; cb < NCB; ++cb) {
         if (cb < cb0 || cb >= cb1) continue;                     // wave-uniform
         tw_compiler_fence();
+        if constexpr (FUSED == kAdd) {
+#pragma unroll
+            for (int i = 0; i < 32 / RPI; ++i) {
+                unsigned char* at = stage + (rr + RPI * i) * PITCH + pc * 16;
+                *(tw_u32x2*)at = tw_u32x2{radd[i].x, radd[i].y};
+                *(tw_u32x2*)(at + 8) = tw_u32x2{radd[i].z, radd[i].w};
+            }
+            tw_compiler_fence();
+            if (cb + 1 < NCB && cb + 1 < cb1) request_add(cb + 1);
+#pragma unroll
+            for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const tw_u32x2 v = *(const tw_u32x2*)(stage + n * PITCH + (32 * ms + 8 * q + 4 * h) * 2);
+                    acc[ms][cb][4 * q + 0] += tw_to_f32<DT>((unsigned short)(v.x & 0xFFFFu));
+                    acc[ms][cb][4 * q + 1] += tw_to_f32<DT>((unsigned short)(v.x >> 16));
+                    acc[ms][cb][4 * q + 2] += tw_to_f32<DT>((unsigned short)(v.y & 0xFFFFu));
+                    acc[ms][cb][4 * q + 3] += tw_to_f32<DT>((unsigned short)(v.y >> 16));
+                }
+            tw_compiler_fence();
+        }
 #pragma unroll
         for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
@@ -940,7 +1073,18 @@ __device__ __forceinline__ void store_tile_t(const TwGemmParams& p, const TileU&
         }
         unsigned v = 0u;
         if constexpr (FUSED) {   // a pruned column holds act(bias) for every token
-            const unsigned hv = tw_cvt<DT>(tw_activate(p.bias != nullptr ? tw_to_f32<DT>(p.bias[col]) : 0.f, p.act));
+            const float base = tw_activate(p.bias != nullptr ? tw_to_f32<DT>(p.bias[col]) : 0.f, p.act);
+            if constexpr (FUSED == kAdd) {
+                const tw_u32x4 a = get_piece((long)col);
+                tw_u32x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    o[e] = (unsigned)tw_cvt<DT>(base + tw_to_f32<DT>((unsigned short)(a[e] & 0xFFFFu))) |
+                           ((unsigned)tw_cvt<DT>(base + tw_to_f32<DT>((unsigned short)(a[e] >> 16))) << 16);
+                put_piece((long)col, o);
+                continue;
+            }
+            const unsigned hv = tw_cvt<DT>(base);
             v = hv | (hv << 16);
         }
         put_piece((long)col, tw_u32x4{v, v, v, v});
@@ -1125,14 +1269,16 @@ __device__ __forceinline__ void xc_request(const TwGemmParams& p, const TileU& d
     x.s1 = fetch_int(xp, 1);
     if (x.s0 != x.s1) request_block_steps<1>(x.r, p.blob + p.off_xm_goff, p.blob + p.off_xm_b, x.s0, x.s1, lane);
 }
-template <int DT, int MS, bool FUSED>
+template <int DT, int MS, int FUSED>
 __device__ __forceinline__ void xc_store(const TwGemmParams& p, const TileU& d, const tw_f32x16 (&acc)[MS][1],
-                                         unsigned short* xbuf, int lane) {
+                                         unsigned short* xbuf, int row0, int lane) {
     const int n = lane & 31, h = lane >> 5;
     if (n < xc_count(d)) {
         float bias = 0.f;
+        const int col = FUSED ? ((const int*)(p.blob + p.off_xc_col))[(d.xc & 0x3FFFFFF) + n] : 0;
+        const int last = block_end(p, row0) - 1;
         if constexpr (FUSED)
-            if (p.bias != nullptr) bias = tw_to_f32<DT>(p.bias[((const int*)(p.blob + p.off_xc_col))[(d.xc & 0x3FFFFFF) + n]]);
+            if (p.bias != nullptr) bias = tw_to_f32<DT>(p.bias[col]);
 #pragma unroll
         for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
@@ -1142,6 +1288,10 @@ __device__ __forceinline__ void xc_store(const TwGemmParams& p, const TileU& d, 
                 for (int q = 0; q < 4; ++q) {
                     v[q] = acc[ms][0][4 * q + i];
                     if constexpr (FUSED) v[q] = tw_activate(v[q] + bias, p.act);
+                    if constexpr (FUSED == kAdd) {
+                        const int r = row0 + 32 * ms + 8 * q + 4 * h + i;
+                        v[q] += tw_to_f32<DT>(p.res[(long)(r < last ? r : last) * p.ldr + col]);
+                    }
                 }
                 tw_u32x2 o;
                 o.x = (unsigned)tw_cvt<DT>(v[0]) | ((unsigned)tw_cvt<DT>(v[1]) << 16);
@@ -1152,23 +1302,29 @@ __device__ __forceinline__ void xc_store(const TwGemmParams& p, const TileU& d, 
 }
 // Transposed boundary: a column is a row of Ct, `xbuf` is [column][token] and the epilogue writes its rows in place
 // of the lines of zeros.
-template <int DT, int MS, bool FUSED>
+template <int DT, int MS, int FUSED>
 __device__ __forceinline__ void xc_store_t(const TwGemmParams& p, const TileU& d, const tw_f32x16 (&acc)[MS][1],
-                                           unsigned short* xbuf, int lane) {
+                                           unsigned short* xbuf, int m0, int lane) {
     const int n = lane & 31, h = lane >> 5;
     if (n < xc_count(d)) {
         float bias = 0.f;
+        const int col = FUSED ? ((const int*)(p.blob + p.off_xc_col))[(d.xc & 0x3FFFFFF) + n] : 0;
         if constexpr (FUSED)
-            if (p.bias != nullptr) bias = tw_to_f32<DT>(p.bias[((const int*)(p.blob + p.off_xc_col))[(d.xc & 0x3FFFFFF) + n]]);
+            if (p.bias != nullptr) bias = tw_to_f32<DT>(p.bias[col]);
 #pragma unroll
         for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {                    // tokens 32*ms + 8*q + 4*h .. + 3
                 float v[4];
+                tw_u32x2 a{0u, 0u};                          // (four tokens of a row lie within its pitch if the first one exists)
+                const int m = m0 + 32 * ms + 8 * q + 4 * h;
+                if constexpr (FUSED == kAdd)
+                    if (m < p.M) a = *(const tw_u32x2*)(p.res + (long)col * p.ldr + m);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     v[i] = acc[ms][0][4 * q + i];
                     if constexpr (FUSED) v[i] = tw_activate(v[i] + bias, p.act);
+                    if constexpr (FUSED == kAdd) v[i] += tw_to_f32<DT>((unsigned short)(a[i >> 1] >> (16 * (i & 1))));
                 }
                 tw_u32x2 o;
                 o.x = (unsigned)tw_cvt<DT>(v[0]) | ((unsigned)tw_cvt<DT>(v[1]) << 16);
@@ -1178,16 +1334,16 @@ __device__ __forceinline__ void xc_store_t(const TwGemmParams& p, const TileU& d
     }
 }
 // K resident: everything at once
-template <int DT, int MS, bool FUSED, bool TRANS>
+template <int DT, int MS, int FUSED, bool TRANS>
 __device__ __forceinline__ void xc_columns(const TwGemmParams& p, const TileU& d, XcSteps& x, const unsigned char* at,
-                                           unsigned at_pitch, unsigned short* xbuf, int lane) {
+                                           unsigned at_pitch, unsigned short* xbuf, int row0, int lane) {
     if (xc_count(d) == 0) return;                            // wave-uniform
     tw_f32x16 acc[MS][1];
     zero_acc<MS, 1>(acc);
     if (x.s0 != x.s1)
         run_block_steps<DT, MS, 1>(acc, x.r, at, at_pitch, p.blob + p.off_xm_goff, p.blob + p.off_xm_b, x.s0, x.s1, lane);
-    if constexpr (TRANS) xc_store_t<DT, MS, FUSED>(p, d, acc, xbuf, lane);
-    else xc_store<DT, MS, FUSED>(p, d, acc, xbuf, lane);
+    if constexpr (TRANS) xc_store_t<DT, MS, FUSED>(p, d, acc, xbuf, row0, lane);
+    else xc_store<DT, MS, FUSED>(p, d, acc, xbuf, row0, lane);
 }
 // K streamed: the sums of the 16 columns between chunks, fp32, piece (ms, q) of lane (h, n < 16) at float offset
 // (((4 * ms + q) * 32 + 16 * h + n) * 4 of `area` (4 KB with 64 rows)
@@ -1231,14 +1387,14 @@ __device__ __forceinline__ void xc_chunk(const TwGemmParams& p, const TileU& d, 
                     tw_f32x4{acc[ms][0][4 * q + 0], acc[ms][0][4 * q + 1], acc[ms][0][4 * q + 2], acc[ms][0][4 * q + 3]};
     }
 }
-template <int DT, int MS, bool FUSED, bool TRANS>
+template <int DT, int MS, int FUSED, bool TRANS>
 __device__ __forceinline__ void xc_finish(const TwGemmParams& p, const TileU& d, const unsigned char* area,
-                                          unsigned short* xbuf, int lane) {
+                                          unsigned short* xbuf, int row0, int lane) {
     if (xc_count(d) == 0) return;                            // wave-uniform
     tw_f32x16 acc[MS][1];
     xc_load_partial<MS>(acc, area, lane);
-    if constexpr (TRANS) xc_store_t<DT, MS, FUSED>(p, d, acc, xbuf, lane);
-    else xc_store<DT, MS, FUSED>(p, d, acc, xbuf, lane);
+    if constexpr (TRANS) xc_store_t<DT, MS, FUSED>(p, d, acc, xbuf, row0, lane);
+    else xc_store<DT, MS, FUSED>(p, d, acc, xbuf, row0, lane);
 }
 
 // MODE 0: the K extent of a row block of 32*MS rows is resident in LDS, waves pull whole tiles.
@@ -1275,7 +1431,7 @@ __device__ __forceinline__ void dump_partial(float* dst, const tw_f32x16 (&acc)[
 // EW: the variant for TEW blobs.  The code of the element-wise residual costs the kernels without it 1 to 2.5 %
 // (registers: the widest variants sit at the limit of 256), so blobs without a residual run kernels without it.
 // WL: lines of the epilogue's staging windows.
-template <int DT, int MS, int NCB, int MODE, bool FUSED, bool TRANS, bool NTA = true, bool EW = false, int WL = kWinLines>
+template <int DT, int MS, int NCB, int MODE, int FUSED, bool TRANS, bool NTA = true, bool EW = false, int WL = kWinLines>
 __global__ __launch_bounds__(kThreads) void tw_gemm_kernel(const TwGemmParams p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const bool has_ew = EW && p.has_ew != 0;
@@ -1352,7 +1508,7 @@ __global__ __launch_bounds__(kThreads) void tw_gemm_kernel(const TwGemmParams p)
                 StepRegs<NCB> rg;
                 prefetch_first_steps<NCB>(rg, p.blob + p.off_goff + (long)d.first_step * 32,
                                           p.blob + p.off_bvals + (long)d.first_step * NCB * 1024, 0, d.nsteps, lane);
-                if (xbuf != nullptr) xc_columns<DT, MS, FUSED, TRANS>(p, d, xs, smem, at_pitch_of<MS>(), xbuf, lane);
+                if (xbuf != nullptr) xc_columns<DT, MS, FUSED, TRANS>(p, d, xs, smem, at_pitch_of<MS>(), xbuf, row0, lane);
                 tw_f32x16 acc[MS][NCB];
                 zero_acc<MS, NCB>(acc);
                 run_steps<DT, MS, NCB>(acc, rg, smem, at_pitch_of<MS>(), p.blob + p.off_goff + (long)d.first_step * 32,
@@ -1543,7 +1699,7 @@ __global__ __launch_bounds__(kThreads) void tw_gemm_kernel(const TwGemmParams p)
                 __syncthreads();
                 par ^= p.n_chunks & 1;
                 if (active) {
-                    if (xbuf != nullptr) xc_finish<DT, MS, FUSED, TRANS>(p, d, stage, xbuf, lane);
+                    if (xbuf != nullptr) xc_finish<DT, MS, FUSED, TRANS>(p, d, stage, xbuf, row0, lane);
                     if constexpr (TRANS) store_tile_t<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, 0, NCB, xbuf);
                     else store_tile<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, xbuf, xcols);
                 }
@@ -1687,7 +1843,7 @@ __global__ __launch_bounds__(kThreads) void tw_gemm_kernel(const TwGemmParams p)
                 if constexpr (SPLIT) {
                     dump_partial<MS, NCB>(p.partials + ((((long)part * p.n_mblocks + mb) * p.T + ti) * (long)(MS * NCB * 1024)), acc, lane);
                 } else {
-                    if (xbuf != nullptr) xc_finish<DT, MS, FUSED, TRANS>(p, d, stage, xbuf, lane);
+                    if (xbuf != nullptr) xc_finish<DT, MS, FUSED, TRANS>(p, d, stage, xbuf, row0, lane);
                     if constexpr (TRANS) store_tile_t<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, 0, NCB, xbuf);
                     else store_tile<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, xbuf, xcols);
                 }
@@ -1720,7 +1876,7 @@ __global__ __launch_bounds__(kThreads) void tw_gemm_kernel(const TwGemmParams p)
 // The pieces are this small because a compute unit brings in only about 16 KB per microsecond from memory (its
 // queue of outstanding misses times the latency): a wave that summed a whole tile (32 KB per part) would take as
 // long as the chunks it saves.
-template <int DT, int NCB, bool FUSED, bool TRANS>
+template <int DT, int NCB, int FUSED, bool TRANS>
 __global__ __launch_bounds__(64) void tw_splitk_reduce_kernel(const TwGemmParams p) {
     constexpr int MS = 2;
     constexpr int SUB = TRANS ? NCB : 4 * MS;               // pieces per tile
@@ -1860,7 +2016,7 @@ __device__ __forceinline__ void team_sum(const unsigned char* piece, tw_f32x4 (&
 // and the fp32 sums meet in LDS: every wave leaves its own there, and pass by pass (column block by column block on
 // the transposed boundary) the team's waves add them in the order of the steps and store their share of the tile.
 // The order of the sums depends on the plan only, so repeated calls are bit-identical.
-template <int DT, int NCB, bool FUSED, bool TRANS>
+template <int DT, int NCB, int FUSED, bool TRANS>
 __global__ __launch_bounds__(kThreads) void tw_team_kernel(const TwGemmParams p) {
     constexpr int MS = 1;
     constexpr bool PAIR = kPairResident;
@@ -2002,7 +2158,7 @@ constexpr int kRowsStoreArea = 32 * (64 * 2 + 8);
 static_assert(4 * kRowsStoreArea <= 4 * rows_stage_bytes<4>() && 4 * kRowsStoreArea <= 4 * rows_stage_bytes<1>(),
               "the epilogue's staging areas lie over the ring");
 
-template <int DT, int NCB, bool FUSED, int kRowsStages>
+template <int DT, int NCB, int FUSED, int kRowsStages>
 __global__ __launch_bounds__(256, kRowsStages == 4 ? 4 : 2) void tw_rows_kernel(const TwGemmParams p) {
     constexpr int BT = rows_bt<NCB>(), CB = NCB == 4 ? 2 : NCB, IA = BT / 128, STAGE = rows_stage_bytes<NCB>(), A_BYTES = BT * 32;
     constexpr int kLoads = IA + 1;                           // requests of a wave per stage
@@ -2173,7 +2329,7 @@ constexpr unsigned kWindowBytes = 64 * kWindow * 2;
 constexpr unsigned kStreamRange = 0x80000000u;
 static_assert(kStreamChunk % kWindow == 0, "whole windows");
 
-template <int DT, int NCB, bool FUSED>
+template <int DT, int NCB, int FUSED>
 __global__ __launch_bounds__(kThreads) void tw_stream_kernel(const TwGemmParams p) {
     constexpr unsigned PITCH = at_pitch_of<2>();
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -2372,19 +2528,19 @@ __global__ __launch_bounds__(kThreads) void tw_part_kernel(const TwGemmParams p)
 namespace tw_parts {
 // (nta: the streamed kernels' variant whose requests for activations carry the streaming hint)
 // (EW: the variant with the code of the element-wise residual, for TEW blobs)
-template <int DT, bool FUSED, bool EW> const void* pick_mode(int mode, int ms, int ncb, bool nta);     // row-major boundary
-template <int DT, bool FUSED, bool EW> const void* pick_mode_t(int mode, int ms, int ncb, bool nta);   // transposed boundary
-template <int DT, bool FUSED> const void* pick_reduce(int ncb, bool transposed);               // second kernel of split K
-template <int DT, bool FUSED> const void* pick_team(int ncb, bool transposed);                 // teams of waves per tile
-template <int DT, bool FUSED> const void* pick_narrow(int ncb);                                // K resident, 64 rows, narrow staging windows
+template <int DT, int FUSED, bool EW> const void* pick_mode(int mode, int ms, int ncb, bool nta);     // row-major boundary
+template <int DT, int FUSED, bool EW> const void* pick_mode_t(int mode, int ms, int ncb, bool nta);   // transposed boundary
+template <int DT, int FUSED> const void* pick_reduce(int ncb, bool transposed);               // second kernel of split K
+template <int DT, int FUSED> const void* pick_team(int ncb, bool transposed);                 // teams of waves per tile
+template <int DT, int FUSED> const void* pick_narrow(int ncb);                                // K resident, 64 rows, narrow staging windows
 template <int DT> const void* pick_part(int ncb, int tiles);                                    // split K, row-major
-template <int DT, bool FUSED> const void* pick_stream(int ncb);                     // K streamed, row-major
-template <int DT, bool FUSED> const void* pick_rows(int ncb, int stages);                                  // a tile of a token block per workgroup
+template <int DT, int FUSED> const void* pick_stream(int ncb);                     // K streamed, row-major
+template <int DT, int FUSED> const void* pick_rows(int ncb, int stages);                                  // a tile of a token block per workgroup
 }  // namespace tw_parts
 
 #if !defined(TW_PART) || TW_PART != 0
 namespace {
-template <int DT, int MS, int MODE, bool FUSED, bool TRANS, bool EW, bool NTA = true>
+template <int DT, int MS, int MODE, int FUSED, bool TRANS, bool EW, bool NTA = true>
 const void* pick_ncb(int ncb) {
     switch (ncb) {
         case 1: return (const void*)tw_gemm_kernel<DT, MS, 1, MODE, FUSED, TRANS, NTA, EW>;
@@ -2395,30 +2551,30 @@ const void* pick_ncb(int ncb) {
 }
 }  // namespace
 namespace tw_parts {
-template <int DT, bool FUSED, bool EW>
+template <int DT, int FUSED, bool EW>
 const void* pick_mode(int mode, int ms, int ncb, bool nta) {
     if (mode == 0) return ms == 2 ? pick_ncb<DT, 2, 0, FUSED, false, EW>(ncb) : pick_ncb<DT, 1, 0, FUSED, false, EW>(ncb);
     if (ms != 2) return nullptr;                  // the streamed kernels take 64-row blocks
     if (mode == 1) return nta ? pick_ncb<DT, 2, 1, FUSED, false, EW, true>(ncb) : pick_ncb<DT, 2, 1, FUSED, false, EW, false>(ncb);
     if (mode == 3) {                              // split K: the epilogue is the second kernel's, so only the plain variant exists
-        if constexpr (!FUSED) return nta ? pick_ncb<DT, 2, 3, false, false, EW, true>(ncb) : pick_ncb<DT, 2, 3, false, false, EW, false>(ncb);
+        if constexpr (!FUSED) return nta ? pick_ncb<DT, 2, 3, kPlain, false, EW, true>(ncb) : pick_ncb<DT, 2, 3, kPlain, false, EW, false>(ncb);
         else return nullptr;
     }
     return nta ? pick_ncb<DT, 2, 2, FUSED, false, EW, true>(ncb) : pick_ncb<DT, 2, 2, FUSED, false, EW, false>(ncb);
 }
 // transposed boundary: resident K with blocks of 64 or 32 tokens, streamed K always with 64
-template <int DT, bool FUSED, bool EW>
+template <int DT, int FUSED, bool EW>
 const void* pick_mode_t(int mode, int ms, int ncb, bool nta) {
     if (mode == 0) return ms == 2 ? pick_ncb<DT, 2, 0, FUSED, true, EW>(ncb) : pick_ncb<DT, 1, 0, FUSED, true, EW>(ncb);
     if (ms != 2) return nullptr;
     if (mode == 1) return nta ? pick_ncb<DT, 2, 1, FUSED, true, EW, true>(ncb) : pick_ncb<DT, 2, 1, FUSED, true, EW, false>(ncb);
     if (mode == 3) {
-        if constexpr (!FUSED) return nta ? pick_ncb<DT, 2, 3, false, true, EW, true>(ncb) : pick_ncb<DT, 2, 3, false, true, EW, false>(ncb);
+        if constexpr (!FUSED) return nta ? pick_ncb<DT, 2, 3, kPlain, true, EW, true>(ncb) : pick_ncb<DT, 2, 3, kPlain, true, EW, false>(ncb);
         else return nullptr;
     }
     return nta ? pick_ncb<DT, 2, 2, FUSED, true, EW, true>(ncb) : pick_ncb<DT, 2, 2, FUSED, true, EW, false>(ncb);
 }
-template <int DT, bool FUSED>
+template <int DT, int FUSED>
 const void* pick_reduce(int ncb, bool transposed) {
     switch (ncb) {
         case 1: return transposed ? (const void*)tw_splitk_reduce_kernel<DT, 1, FUSED, true> : (const void*)tw_splitk_reduce_kernel<DT, 1, FUSED, false>;
@@ -2427,7 +2583,7 @@ const void* pick_reduce(int ncb, bool transposed) {
         default: return nullptr;
     }
 }
-template <int DT, bool FUSED>
+template <int DT, int FUSED>
 const void* pick_narrow(int ncb) {
     switch (ncb) {
         case 1: return (const void*)tw_gemm_kernel<DT, 2, 1, 0, FUSED, false, true, false, kNarrowLines>;
@@ -2445,7 +2601,7 @@ const void* pick_part(int ncb, int tiles) {
         default: return nullptr;
     }
 }
-template <int DT, bool FUSED>
+template <int DT, int FUSED>
 const void* pick_stream(int ncb) {
     switch (ncb) {
         case 1: return (const void*)tw_stream_kernel<DT, 1, FUSED>;
@@ -2454,7 +2610,7 @@ const void* pick_stream(int ncb) {
         default: return nullptr;
     }
 }
-template <int DT, bool FUSED>
+template <int DT, int FUSED>
 const void* pick_rows(int ncb, int stages) {
     switch (ncb) {
         case 1: return stages == 4 ? (const void*)tw_rows_kernel<DT, 1, FUSED, 4> : (const void*)tw_rows_kernel<DT, 1, FUSED, 8>;
@@ -2463,7 +2619,7 @@ const void* pick_rows(int ncb, int stages) {
         default: return nullptr;
     }
 }
-template <int DT, bool FUSED>
+template <int DT, int FUSED>
 const void* pick_team(int ncb, bool transposed) {
     switch (ncb) {
         case 1: return transposed ? (const void*)tw_team_kernel<DT, 1, FUSED, true> : (const void*)tw_team_kernel<DT, 1, FUSED, false>;
@@ -2489,50 +2645,61 @@ const void* pick_team(int ncb, bool transposed) {
 #define TW_TABLES_PART(KW, DT) KW template const void* tw_parts::pick_part<DT>(int, int);
 #if TW_PART == 0
 TW_TABLES_PART(extern, TW_F16) TW_TABLES_PART(extern, TW_BF16)
-TW_TABLES_ALL(extern, TW_F16, false) TW_TABLES_ALL(extern, TW_F16, true) TW_TABLES_ALL(extern, TW_BF16, false) TW_TABLES_ALL(extern, TW_BF16, true)
+TW_TABLES_ALL(extern, TW_F16, 0) TW_TABLES_ALL(extern, TW_F16, 1) TW_TABLES_ALL(extern, TW_F16, 2)
+TW_TABLES_ALL(extern, TW_BF16, 0) TW_TABLES_ALL(extern, TW_BF16, 1) TW_TABLES_ALL(extern, TW_BF16, 2)
 #elif TW_PART == 1
-TW_TABLES_EW(, TW_F16, false, false) TW_TABLES_REDUCE(, TW_F16, false) TW_TABLES_PART(, TW_F16)
+TW_TABLES_EW(, TW_F16, 0, false) TW_TABLES_REDUCE(, TW_F16, 0) TW_TABLES_PART(, TW_F16)
 #elif TW_PART == 2
-TW_TABLES_EW(, TW_F16, true, false) TW_TABLES_REDUCE(, TW_F16, true)
+TW_TABLES_EW(, TW_F16, 1, false) TW_TABLES_REDUCE(, TW_F16, 1)
 #elif TW_PART == 3
-TW_TABLES_EW(, TW_BF16, false, false) TW_TABLES_REDUCE(, TW_BF16, false) TW_TABLES_PART(, TW_BF16)
+TW_TABLES_EW(, TW_BF16, 0, false) TW_TABLES_REDUCE(, TW_BF16, 0) TW_TABLES_PART(, TW_BF16)
 #elif TW_PART == 4
-TW_TABLES_EW(, TW_BF16, true, false) TW_TABLES_REDUCE(, TW_BF16, true)
+TW_TABLES_EW(, TW_BF16, 1, false) TW_TABLES_REDUCE(, TW_BF16, 1)
 #elif TW_PART == 5
-TW_TABLES_EW(, TW_F16, false, true)
+TW_TABLES_EW(, TW_F16, 0, true)
 #elif TW_PART == 6
-TW_TABLES_EW(, TW_F16, true, true)
+TW_TABLES_EW(, TW_F16, 1, true)
 #elif TW_PART == 7
-TW_TABLES_EW(, TW_BF16, false, true)
+TW_TABLES_EW(, TW_BF16, 0, true)
 #elif TW_PART == 8
-TW_TABLES_EW(, TW_BF16, true, true)
+TW_TABLES_EW(, TW_BF16, 1, true)
+#elif TW_PART == 9
+TW_TABLES_EW(, TW_F16, 2, false) TW_TABLES_REDUCE(, TW_F16, 2)
+#elif TW_PART == 10
+TW_TABLES_EW(, TW_BF16, 2, false) TW_TABLES_REDUCE(, TW_BF16, 2)
+#elif TW_PART == 11
+TW_TABLES_EW(, TW_F16, 2, true)
+#elif TW_PART == 12
+TW_TABLES_EW(, TW_BF16, 2, true)
 #else
-#error "TW_PART is 0 (host code) or 1..8 (kernels)"
+#error "TW_PART is 0 (host code) or 1..12 (kernels)"
 #endif
 #endif
 
 #if !defined(TW_PART) || TW_PART == 0
 namespace {
 
-// C[m, n] = act(bias[n]) (zero without a bias) for a weight with no surviving column.
+// C[m, n] = act(bias[n]) (zero without a bias) for a weight with no surviving column, plus what is added.
 template <int DT>
-__global__ void tw_fill_kernel(unsigned short* C, long ldc, int M, int N, const unsigned short* bias, int act) {
+__global__ void tw_fill_kernel(unsigned short* C, long ldc, int M, int N, const unsigned short* bias, int act, const unsigned short* res, long ldr) {
     const long n = (long)blockIdx.x * blockDim.x + threadIdx.x;
     const long total = (long)M * N;
     for (long i = n; i < total; i += (long)gridDim.x * blockDim.x) {
         const long col = i % N;
-        C[(i / N) * ldc + col] = bias ? tw_cvt<DT>(tw_activate(tw_to_f32<DT>(bias[col]), act)) : (unsigned short)0;
+        const float x = bias ? tw_activate(tw_to_f32<DT>(bias[col]), act) : 0.f;
+        C[(i / N) * ldc + col] = tw_cvt<DT>(res ? x + tw_to_f32<DT>(res[(i / N) * ldr + col]) : x);
     }
 }
 
-// Ct[n, m] = act(bias[n]) (zero without a bias): the transposed output of a weight with no surviving column.
+// Ct[n, m] = act(bias[n]) (zero without a bias): the transposed output of a weight with no surviving column, plus what is added.
 template <int DT>
-__global__ void tw_fill_rows_kernel(unsigned short* Ct, long ldct, int N, int M, const unsigned short* bias, int act) {
+__global__ void tw_fill_rows_kernel(unsigned short* Ct, long ldct, int N, int M, const unsigned short* bias, int act, const unsigned short* res, long ldr) {
     const long t = (long)blockIdx.x * blockDim.x + threadIdx.x;
     const long total = (long)N * M;
     for (long i = t; i < total; i += (long)gridDim.x * blockDim.x) {
         const long n = i / M;
-        Ct[n * ldct + (i % M)] = bias ? tw_cvt<DT>(tw_activate(tw_to_f32<DT>(bias[n]), act)) : (unsigned short)0;
+        const float x = bias ? tw_activate(tw_to_f32<DT>(bias[n]), act) : 0.f;
+        Ct[n * ldct + (i % M)] = tw_cvt<DT>(res ? x + tw_to_f32<DT>(res[n * ldr + (i % M)]) : x);
     }
 }
 
@@ -2550,7 +2717,8 @@ struct XcolParams {
     const int* k;
     const unsigned short* v;
     const int* rank;            // position of a column among those of its tile
-    long lda, ldc;
+    const unsigned short* res;  // added behind the activation (pitch ldr), or null
+    long lda, ldc, ldr;
     int M, K, n_cols, act;
     int skip_below;             // columns with rank < skip_below were added by the tiles' kernel already
 };
@@ -2658,7 +2826,9 @@ __global__ __launch_bounds__(256) void tw_xcol_kernel(const XcolParams p) {
             if (j < p.n_cols && p.rank[j] >= p.skip_below) {
                 const int n = p.col[j];
                 const float b = p.bias ? tw_to_f32<DT>(p.bias[n]) : 0.f;
-                p.C[(long)m * p.ldc + n] = tw_cvt<DT>(tw_activate(acc[i] + b, p.act));
+                float x = tw_activate(acc[i] + b, p.act);
+                if (p.res) x += tw_to_f32<DT>(p.res[(long)m * p.ldr + n]);
+                p.C[(long)m * p.ldc + n] = tw_cvt<DT>(x);
             }
         }
     }
@@ -2688,13 +2858,15 @@ __global__ __launch_bounds__(256) void tw_xcol_t_kernel(const XcolParams p) {
             acc += tw_to_f32<DT>(p.v[e]) * tw_to_f32<DT>(p.A[(long)p.k[e] * p.lda + m]);
         const int n = p.col[j];
         const float b = p.bias ? tw_to_f32<DT>(p.bias[n]) : 0.f;
-        p.C[(long)n * p.ldc + m] = tw_cvt<DT>(tw_activate(acc + b, p.act));
+        float x = tw_activate(acc + b, p.act);
+        if (p.res) x += tw_to_f32<DT>(p.res[(long)n * p.ldr + m]);
+        p.C[(long)n * p.ldc + m] = tw_cvt<DT>(x);
     }
 }
 
 // Enqueues the pass over the residual's columns without tile-wise weights, if the blob has any.
 int launch_xcols(const TwHeader* h, const void* blob_dev, const void* A, long lda, void* C, long ldc, int M,
-                 const void* bias, int act, bool transposed, hipStream_t stream, bool inline_done = false) {
+                 const void* bias, int act, const void* res, long ldr, bool transposed, hipStream_t stream, bool inline_done = false) {
     if (h->xc_n <= 0 || M <= 0) return TW_OK;
     if (inline_done && h->xc_overflow == 0) return TW_OK;   // the tiles' kernel added them all
     const unsigned char* b = (const unsigned char*)blob_dev;
@@ -2703,7 +2875,8 @@ int launch_xcols(const TwHeader* h, const void* blob_dev, const void* A, long ld
     p.col = (const int*)(b + h->off_xc_col); p.ptr = (const int*)(b + h->off_xc_ptr);
     p.k = (const int*)(b + h->off_xc_k); p.v = (const unsigned short*)(b + h->off_xc_v);
     p.rank = (const int*)(b + h->off_xc_rank);
-    p.lda = lda; p.ldc = ldc; p.M = M; p.K = h->K; p.n_cols = h->xc_n; p.act = act;
+    p.res = (const unsigned short*)res;
+    p.lda = lda; p.ldc = ldc; p.ldr = ldr; p.M = M; p.K = h->K; p.n_cols = h->xc_n; p.act = act;
     p.skip_below = inline_done ? TW_XC_INLINE : 0;
     void* args[] = {(void*)&p};
     hipError_t rc;
@@ -3096,49 +3269,55 @@ bool parts_by_direct_loads(const TwHeader* h, long lda, const Plan& pl) {
 unsigned part_lds_bytes() { return at_bytes(2, kStreamChunk) + 2 * 64 * kStreamChunk * 2; }
 
 // the kernel for (dtype, mode, MS, NCB, fused epilogue): a host-side address for hipLaunchKernel and hipFuncSetAttribute
-template <bool EW>
-const void* pick_kernel_t_of(int dt, int mode, int ms, int ncb, bool fused, bool nta) {
+template <int EPI, bool EW>
+const void* pick_tile_kernel(int dt, int mode, int ms, int ncb, bool nta, bool transposed) {
     using namespace tw_parts;
-    if (fused) return dt == TW_F16 ? pick_mode_t<TW_F16, true, EW>(mode, ms, ncb, nta) : pick_mode_t<TW_BF16, true, EW>(mode, ms, ncb, nta);
-    return dt == TW_F16 ? pick_mode_t<TW_F16, false, EW>(mode, ms, ncb, nta) : pick_mode_t<TW_BF16, false, EW>(mode, ms, ncb, nta);
+    if (transposed) return dt == TW_F16 ? pick_mode_t<TW_F16, EPI, EW>(mode, ms, ncb, nta) : pick_mode_t<TW_BF16, EPI, EW>(mode, ms, ncb, nta);
+    return dt == TW_F16 ? pick_mode<TW_F16, EPI, EW>(mode, ms, ncb, nta) : pick_mode<TW_BF16, EPI, EW>(mode, ms, ncb, nta);
 }
-template <bool EW>
-const void* pick_kernel_of(int dt, int mode, int ms, int ncb, bool fused, bool nta) {
-    using namespace tw_parts;
-    if (fused) return dt == TW_F16 ? pick_mode<TW_F16, true, EW>(mode, ms, ncb, nta) : pick_mode<TW_BF16, true, EW>(mode, ms, ncb, nta);
-    return dt == TW_F16 ? pick_mode<TW_F16, false, EW>(mode, ms, ncb, nta) : pick_mode<TW_BF16, false, EW>(mode, ms, ncb, nta);
+// f(epilogue variant as a constant): kPlain, kFused or kAdd
+template <class F>
+const void* by_epilogue(int epi, F f) {
+    if (epi == kAdd) return f(std::integral_constant<int, kAdd>{});
+    if (epi == kFused) return f(std::integral_constant<int, kFused>{});
+    return f(std::integral_constant<int, kPlain>{});
 }
 // (ew: the blob carries an element-wise residual)
-const void* pick_kernel_t(int dt, int mode, int ms, int ncb, bool fused, bool nta, bool ew) {
-    return ew ? pick_kernel_t_of<true>(dt, mode, ms, ncb, fused, nta) : pick_kernel_t_of<false>(dt, mode, ms, ncb, fused, nta);
+const void* pick_kernel(int dt, int mode, int ms, int ncb, int epi, bool nta, bool ew, bool transposed) {
+    return by_epilogue(epi, [&](auto e) {
+        constexpr int E = decltype(e)::value;
+        return ew ? pick_tile_kernel<E, true>(dt, mode, ms, ncb, nta, transposed) : pick_tile_kernel<E, false>(dt, mode, ms, ncb, nta, transposed);
+    });
 }
-const void* pick_kernel(int dt, int mode, int ms, int ncb, bool fused, bool nta, bool ew) {
-    return ew ? pick_kernel_of<true>(dt, mode, ms, ncb, fused, nta) : pick_kernel_of<false>(dt, mode, ms, ncb, fused, nta);
+const void* pick_team_kernel(int dt, int ncb, int epi, bool transposed) {
+    return by_epilogue(epi, [&](auto e) {
+        constexpr int E = decltype(e)::value;
+        return dt == TW_F16 ? tw_parts::pick_team<TW_F16, E>(ncb, transposed) : tw_parts::pick_team<TW_BF16, E>(ncb, transposed);
+    });
 }
-const void* pick_team_kernel(int dt, int ncb, bool fused, bool transposed) {
-    using namespace tw_parts;
-    if (fused) return dt == TW_F16 ? pick_team<TW_F16, true>(ncb, transposed) : pick_team<TW_BF16, true>(ncb, transposed);
-    return dt == TW_F16 ? pick_team<TW_F16, false>(ncb, transposed) : pick_team<TW_BF16, false>(ncb, transposed);
+const void* pick_narrow_kernel(int dt, int ncb, int epi) {
+    return by_epilogue(epi, [&](auto e) {
+        constexpr int E = decltype(e)::value;
+        return dt == TW_F16 ? tw_parts::pick_narrow<TW_F16, E>(ncb) : tw_parts::pick_narrow<TW_BF16, E>(ncb);
+    });
 }
-const void* pick_narrow_kernel(int dt, int ncb, bool fused) {
-    using namespace tw_parts;
-    if (fused) return dt == TW_F16 ? pick_narrow<TW_F16, true>(ncb) : pick_narrow<TW_BF16, true>(ncb);
-    return dt == TW_F16 ? pick_narrow<TW_F16, false>(ncb) : pick_narrow<TW_BF16, false>(ncb);
+const void* pick_stream_kernel(int dt, int ncb, int epi) {
+    return by_epilogue(epi, [&](auto e) {
+        constexpr int E = decltype(e)::value;
+        return dt == TW_F16 ? tw_parts::pick_stream<TW_F16, E>(ncb) : tw_parts::pick_stream<TW_BF16, E>(ncb);
+    });
 }
-const void* pick_stream_kernel(int dt, int ncb, bool fused) {
-    using namespace tw_parts;
-    if (fused) return dt == TW_F16 ? pick_stream<TW_F16, true>(ncb) : pick_stream<TW_BF16, true>(ncb);
-    return dt == TW_F16 ? pick_stream<TW_F16, false>(ncb) : pick_stream<TW_BF16, false>(ncb);
+const void* pick_rows_kernel(int dt, int ncb, int epi, int stages) {
+    return by_epilogue(epi, [&](auto e) {
+        constexpr int E = decltype(e)::value;
+        return dt == TW_F16 ? tw_parts::pick_rows<TW_F16, E>(ncb, stages) : tw_parts::pick_rows<TW_BF16, E>(ncb, stages);
+    });
 }
-const void* pick_rows_kernel(int dt, int ncb, bool fused, int stages) {
-    using namespace tw_parts;
-    if (fused) return dt == TW_F16 ? pick_rows<TW_F16, true>(ncb, stages) : pick_rows<TW_BF16, true>(ncb, stages);
-    return dt == TW_F16 ? pick_rows<TW_F16, false>(ncb, stages) : pick_rows<TW_BF16, false>(ncb, stages);
-}
-const void* pick_reduce_kernel(int dt, int ncb, bool fused, bool transposed) {
-    using namespace tw_parts;
-    if (fused) return dt == TW_F16 ? pick_reduce<TW_F16, true>(ncb, transposed) : pick_reduce<TW_BF16, true>(ncb, transposed);
-    return dt == TW_F16 ? pick_reduce<TW_F16, false>(ncb, transposed) : pick_reduce<TW_BF16, false>(ncb, transposed);
+const void* pick_reduce_kernel(int dt, int ncb, int epi, bool transposed) {
+    return by_epilogue(epi, [&](auto e) {
+        constexpr int E = decltype(e)::value;
+        return dt == TW_F16 ? tw_parts::pick_reduce<TW_F16, E>(ncb, transposed) : tw_parts::pick_reduce<TW_BF16, E>(ncb, transposed);
+    });
 }
 
 // Per-device facts looked up once (the entries are written with the same value by every thread
@@ -3161,7 +3340,8 @@ int device_cus(int dev) {
 }
 
 // The dynamic-LDS limit of a kernel is raised to the hardware maximum once per (device, kernel).
-constexpr int kMaxKernels = 560;
+constexpr int kKernels = 560;               // numbers of the plain and the fused variants; those that add follow
+constexpr int kMaxKernels = 2 * kKernels;
 std::atomic<unsigned> g_lds_set[kMaxDevices][kMaxKernels];
 
 int ensure_lds(int dev, int kernel_id, const void* fn) {
@@ -3253,6 +3433,10 @@ int check_gemm_args(const void* blob_host, const void* blob_dev, const void* A, 
     return TW_OK;
 }
 
+// R and C may be one matrix (an element is read by the lane that writes it, before it does), except where a second kernel adds the
+// residual weights' own columns: the first has then written them already.
+bool adds_to_itself_twice(const TwHeader* h, const void* R, const void* C) { return R == C && h->xc_n > 0; }
+
 // ---- scratch memory of the entry point that allocates nothing and takes no workspace (tw_gemm_static) ----
 // The scheduler's counters (its first 256 bytes) and the fp32 partial results of a split-K plan (the rest; the
 // planner takes a split only if they fit) live in this array instead of a buffer of the caller.  Only the counters
@@ -3298,16 +3482,11 @@ extern "C" int tw_gemm_static(const void* blob_host, const void* blob_dev, const
                             hip_stream);
 }
 
-extern "C" int tw_gemm_bias_act(const void* blob_host, const void* blob_dev, const void* A, int M, int lda,
-                                const void* bias, tw_act act, void* C, int ldc, void* workspace, size_t ws_bytes,
-                                void* hip_stream) {
-    {
-        const int rc0 = check_gemm_args(blob_host, blob_dev, A, M, lda, bias, act, C, ldc, workspace, ws_bytes);
-        if (rc0) return rc0;
-    }
+namespace {
+// tw_gemm_bias_act and, with a matrix to add (R), tw_gemm_bias_act_add; the arguments have been checked, M > 0
+int run_gemm(const void* blob_host, const void* blob_dev, const void* A, int M, int lda, const void* bias, tw_act act, const void* R, int ldr,
+             void* C, int ldc, void* workspace, size_t ws_bytes, hipStream_t stream) {
     const TwHeader* h = (const TwHeader*)blob_host;
-    if (M == 0) return TW_OK;
-    hipStream_t stream = (hipStream_t)hip_stream;
 
     if (h->T == 0) {
         const long total = (long)M * h->N;
@@ -3317,10 +3496,12 @@ extern "C" int tw_gemm_bias_act(const void* blob_host, const void* blob_dev, con
         long ldc_ = ldc;
         int m_ = M, n_ = h->N, act_ = (int)act;
         const unsigned short* bias_ = (const unsigned short*)bias;
-        void* fargs[] = {(void*)&c_, (void*)&ldc_, (void*)&m_, (void*)&n_, (void*)&bias_, (void*)&act_};
+        const unsigned short* r_ = (const unsigned short*)R;
+        long ldr_ = ldr;
+        void* fargs[] = {(void*)&c_, (void*)&ldc_, (void*)&m_, (void*)&n_, (void*)&bias_, (void*)&act_, (void*)&r_, (void*)&ldr_};
         const void* ffn = h->dtype == TW_F16 ? (const void*)tw_fill_kernel<TW_F16> : (const void*)tw_fill_kernel<TW_BF16>;
         if (hipLaunchKernel(ffn, dim3(blocks), dim3(256), fargs, 0, stream) != hipSuccess) return TW_ERR_HIP;
-        return launch_xcols(h, blob_dev, A, lda, C, ldc, M, bias, (int)act, false, stream);
+        return launch_xcols(h, blob_dev, A, lda, C, ldc, M, bias, (int)act, R, ldr, false, stream);
     }
 
     const int dev = current_device();
@@ -3332,8 +3513,9 @@ extern "C" int tw_gemm_bias_act(const void* blob_host, const void* blob_dev, con
     if (rc) return rc;
     plan_stream(h, lda, pl);
     const bool split = pl.n_parts > 1;
-    const bool fused_epilogue = bias != nullptr || act != TW_ACT_NONE;
-    const bool fused = fused_epilogue && !split;      // split K: the epilogue is the second kernel's
+    const int epilogue = R != nullptr ? kAdd : bias != nullptr || act != TW_ACT_NONE ? kFused : kPlain;
+    const int epi = split ? kPlain : epilogue;        // split K: the epilogue is the second kernel's
+    const bool fused = epi != kPlain;
     // streamed K: the activations carry the streaming hint only when one workgroup reads a row block's rows
     const bool nta = pl.mode == 0 || pl.n_seg == 1;
     const int kmode = split ? 3 : pl.mode;             // the kernel's MODE
@@ -3343,7 +3525,7 @@ extern "C" int tw_gemm_bias_act(const void* blob_host, const void* blob_dev, con
     int kernel_id;
     unsigned lds_bytes = pl.lds_bytes;
     if (pl.stream_items > 0) {
-        fn = pick_stream_kernel(h->dtype, h->ncb, fused);
+        fn = pick_stream_kernel(h->dtype, h->ncb, epi);
         kernel_id = 492 + (bf16 ? 6 : 0) + (fused ? 3 : 0) + (h->ncb >> 1);
         lds_bytes = stream_lds_bytes();
     } else if (parts_by_direct_loads(h, lda, pl)) {
@@ -3351,20 +3533,20 @@ extern "C" int tw_gemm_bias_act(const void* blob_host, const void* blob_dev, con
         kernel_id = 528 + (bf16 ? 9 : 0) + (pl.tiles_per_set <= 2 ? 0 : pl.tiles_per_set <= 4 ? 3 : 6) + (h->ncb >> 1);
         lds_bytes = part_lds_bytes();
     } else if (pl.narrow) {
-        fn = pick_narrow_kernel(h->dtype, h->ncb, fused);
+        fn = pick_narrow_kernel(h->dtype, h->ncb, epi);
         kernel_id = 516 + (bf16 ? 6 : 0) + (fused ? 3 : 0) + (h->ncb >> 1);
     } else {
         const bool team = pl.team_shift > 0;
-        fn = team ? pick_team_kernel(h->dtype, h->ncb, fused, false) : pick_kernel(h->dtype, kmode, pl.ms, h->ncb, fused, nta, h->ew_nnz > 0);
+        fn = team ? pick_team_kernel(h->dtype, h->ncb, epi, false) : pick_kernel(h->dtype, kmode, pl.ms, h->ncb, epi, nta, h->ew_nnz > 0, false);
         kernel_id = tile_kernel_id(h, pl, kmode, fused, nta, false);
     }
     if (!fn) return TW_ERR_UNSUPPORTED;
     const void* fn_reduce = nullptr;
     if (split) {
-        fn_reduce = pick_reduce_kernel(h->dtype, h->ncb, fused_epilogue, false);
+        fn_reduce = pick_reduce_kernel(h->dtype, h->ncb, epilogue, false);
         if (!fn_reduce) return TW_ERR_UNSUPPORTED;
     }
-    rc = ensure_lds(dev, kernel_id, fn);
+    rc = ensure_lds(dev, kernel_id + (epi == kAdd ? kKernels : 0), fn);
     if (rc) return rc;
 
     TwGemmParams p;
@@ -3373,6 +3555,7 @@ extern "C" int tw_gemm_bias_act(const void* blob_host, const void* blob_dev, con
     p.C = (unsigned short*)C;
     p.counters = (int*)workspace;
     p.bias = (const unsigned short*)bias; p.act = (int)act;
+    p.res = (const unsigned short*)R; p.ldr = ldr;
     p.lda = lda; p.ldc = ldc;
     p.M = M; p.K = h->K; p.N = h->N; p.T = h->T;
     p.k_chunk = h->k_chunk; p.n_chunks = h->n_chunks; p.G = h->G;
@@ -3398,7 +3581,30 @@ extern "C" int tw_gemm_bias_act(const void* blob_host, const void* blob_dev, con
         const long units = (long)pl.n_mblocks * h->T * 8;                 // a wave per pass of a tile
         if (hipLaunchKernel(fn_reduce, dim3((unsigned)units), dim3(64), args, 0, stream) != hipSuccess) return TW_ERR_HIP;
     }
-    return launch_xcols(h, blob_dev, A, lda, C, ldc, M, bias, (int)act, false, stream, pl.xbuf_off != 0);
+    return launch_xcols(h, blob_dev, A, lda, C, ldc, M, bias, (int)act, R, ldr, false, stream, pl.xbuf_off != 0);
+}
+}  // namespace
+
+extern "C" int tw_gemm_bias_act(const void* blob_host, const void* blob_dev, const void* A, int M, int lda,
+                                const void* bias, tw_act act, void* C, int ldc, void* workspace, size_t ws_bytes,
+                                void* hip_stream) {
+    const int rc = check_gemm_args(blob_host, blob_dev, A, M, lda, bias, act, C, ldc, workspace, ws_bytes);
+    if (rc || M == 0) return rc;
+    return run_gemm(blob_host, blob_dev, A, M, lda, bias, act, nullptr, 0, C, ldc, workspace, ws_bytes, (hipStream_t)hip_stream);
+}
+
+extern "C" int tw_gemm_bias_act_add(const void* blob_host, const void* blob_dev, const void* A, int M, int lda,
+                                    const void* bias, tw_act act, const void* R, int ldr, void* C, int ldc, void* workspace,
+                                    size_t ws_bytes, void* hip_stream) {
+    const int rc = check_gemm_args(blob_host, blob_dev, A, M, lda, bias, act, C, ldc, workspace, ws_bytes);
+    if (rc) return rc;
+    const TwHeader* h = (const TwHeader*)blob_host;
+    if (!R || ldr < h->N || (R == C && ldr != ldc)) return TW_ERR_ARG;
+    if (((uintptr_t)R & 1) != 0) return TW_ERR_ALIGN;
+    if (ldr >= (1 << 23)) return TW_ERR_UNSUPPORTED;
+    if (adds_to_itself_twice(h, R, C)) return TW_ERR_UNSUPPORTED;
+    if (M == 0) return TW_OK;
+    return run_gemm(blob_host, blob_dev, A, M, lda, bias, act, R, ldr, C, ldc, workspace, ws_bytes, (hipStream_t)hip_stream);
 }
 
 extern "C" int tw_gemm_t(const void* blob_host, const void* blob_dev, const void* At, int M, int ldat, void* Ct,
@@ -3407,21 +3613,25 @@ extern "C" int tw_gemm_t(const void* blob_host, const void* blob_dev, const void
                               hip_stream);
 }
 
-extern "C" int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, const void* At, int M, int ldat,
-                                  const void* bias, tw_act act, void* Ct, int ldct, void* workspace, size_t ws_bytes,
-                                  void* hip_stream) {
+namespace {
+// what tw_gemm_t and its variants refuse before anything is enqueued
+int check_gemm_t_args(const void* blob_host, const void* blob_dev, const void* At, int M, int ldat, const void* bias, tw_act act,
+                      const void* Ct, int ldct, const void* workspace, size_t ws_bytes) {
     if (!blob_host || !blob_dev || !At || !Ct || !workspace || M < 0) return TW_ERR_ARG;
     if (act != TW_ACT_NONE && act != TW_ACT_RELU && act != TW_ACT_GELU) return TW_ERR_ARG;
     if (((uintptr_t)bias & 1) != 0) return TW_ERR_ALIGN;
-    const bool fused_epilogue = bias != nullptr || act != TW_ACT_NONE;
     const TwHeader* h = (const TwHeader*)blob_host;
     if (h->magic != TW_MAGIC || h->version != TW_FORMAT_VERSION) return TW_ERR_BUF;
     if (ws_bytes < 256) return TW_ERR_BUF;
     if (ldat < M || ldct < M) return TW_ERR_ARG;
     if ((ldat & 7) != 0 || (ldct & 7) != 0 || ((uintptr_t)At & 15) != 0 || ((uintptr_t)Ct & 15) != 0) return TW_ERR_ALIGN;
     if (((uintptr_t)blob_dev & 255) != 0 || ((uintptr_t)workspace & 255) != 0) return TW_ERR_ALIGN;
-    if (M == 0) return TW_OK;
-    hipStream_t stream = (hipStream_t)hip_stream;
+    return TW_OK;
+}
+// tw_gemm_t_bias_act and, with a matrix to add (Rt), tw_gemm_t_bias_act_add; the arguments have been checked, M > 0
+int run_gemm_t(const void* blob_host, const void* blob_dev, const void* At, int M, int ldat, const void* bias, tw_act act, const void* Rt,
+               int ldrt, void* Ct, int ldct, void* workspace, size_t ws_bytes, hipStream_t stream) {
+    const TwHeader* h = (const TwHeader*)blob_host;
 
     if (h->T == 0) {   // every row of Ct is zero
         const long total = (long)h->N * M;
@@ -3431,10 +3641,12 @@ extern "C" int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, c
         long ldc_ = ldct;
         int n_ = h->N, m_ = M, act_ = (int)act;
         const unsigned short* bias_ = (const unsigned short*)bias;
-        void* fargs[] = {(void*)&c_, (void*)&ldc_, (void*)&n_, (void*)&m_, (void*)&bias_, (void*)&act_};
+        const unsigned short* r_ = (const unsigned short*)Rt;
+        long ldr_ = ldrt;
+        void* fargs[] = {(void*)&c_, (void*)&ldc_, (void*)&n_, (void*)&m_, (void*)&bias_, (void*)&act_, (void*)&r_, (void*)&ldr_};
         const void* ffn = h->dtype == TW_F16 ? (const void*)tw_fill_rows_kernel<TW_F16> : (const void*)tw_fill_rows_kernel<TW_BF16>;
         if (hipLaunchKernel(ffn, dim3(blocks), dim3(256), fargs, 0, stream) != hipSuccess) return TW_ERR_HIP;
-        return launch_xcols(h, blob_dev, At, ldat, Ct, ldct, M, bias, (int)act, true, stream);
+        return launch_xcols(h, blob_dev, At, ldat, Ct, ldct, M, bias, (int)act, Rt, ldrt, true, stream);
     }
 
     const int dev = current_device();
@@ -3446,27 +3658,29 @@ extern "C" int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, c
     if (rc) return rc;
     plan_rows(h, M, ldat, n_cu, pl, act == TW_ACT_GELU);
     const bool split = pl.n_parts > 1;
-    const bool fused = fused_epilogue && !split;      // split K: the epilogue is the second kernel's
+    const int epilogue = Rt != nullptr ? kAdd : bias != nullptr || act != TW_ACT_NONE ? kFused : kPlain;
+    const int epi = split ? kPlain : epilogue;        // split K: the epilogue is the second kernel's
+    const bool fused = epi != kPlain;
     const bool nta = pl.mode == 0 || pl.n_seg == 1;
     const int kmode = split ? 3 : pl.mode;             // the kernel's MODE
     // the kernel that runs and its number among those whose on-chip memory limit is raised once
     const void* fn;
     int kernel_id;
     if (pl.rows_group > 0) {
-        fn = pick_rows_kernel(h->dtype, h->ncb, fused, pl.rows_stages);
+        fn = pick_rows_kernel(h->dtype, h->ncb, epi, pl.rows_stages);
         kernel_id = pl.rows_stages == 8 ? 480 + (fused ? 6 : 0) + (h->dtype == TW_F16 ? 0 : 3) + (h->ncb >> 1) : -1;   // (at most 64 KB with four)
     } else {
         const bool team = pl.team_shift > 0;
-        fn = team ? pick_team_kernel(h->dtype, h->ncb, fused, true) : pick_kernel_t(h->dtype, kmode, pl.ms, h->ncb, fused, nta, h->ew_nnz > 0);
+        fn = team ? pick_team_kernel(h->dtype, h->ncb, epi, true) : pick_kernel(h->dtype, kmode, pl.ms, h->ncb, epi, nta, h->ew_nnz > 0, true);
         kernel_id = tile_kernel_id(h, pl, kmode, fused, nta, true);
     }
     if (!fn) return TW_ERR_UNSUPPORTED;
     const void* fn_reduce = nullptr;
     if (split) {
-        fn_reduce = pick_reduce_kernel(h->dtype, h->ncb, fused_epilogue, true);
+        fn_reduce = pick_reduce_kernel(h->dtype, h->ncb, epilogue, true);
         if (!fn_reduce) return TW_ERR_UNSUPPORTED;
     }
-    if (kernel_id >= 0) rc = ensure_lds(dev, kernel_id, fn);
+    if (kernel_id >= 0) rc = ensure_lds(dev, kernel_id + (epi == kAdd ? kKernels : 0), fn);
     if (rc) return rc;
 
     TwGemmParams p;
@@ -3475,6 +3689,7 @@ extern "C" int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, c
     p.C = (unsigned short*)Ct;
     p.counters = (int*)workspace;
     p.bias = (const unsigned short*)bias; p.act = (int)act;
+    p.res = (const unsigned short*)Rt; p.ldr = ldrt;
     p.lda = ldat; p.ldc = ldct;
     p.M = M; p.K = h->K; p.N = h->N; p.T = h->T;
     p.k_chunk = h->k_chunk; p.n_chunks = h->n_chunks; p.G = h->G;
@@ -3506,7 +3721,29 @@ extern "C" int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, c
         const long units = (long)pl.n_mblocks * h->T * h->ncb;            // a wave per column block of a tile
         if (hipLaunchKernel(fn_reduce, dim3((unsigned)units), dim3(64), args, 0, stream) != hipSuccess) return TW_ERR_HIP;
     }
-    return launch_xcols(h, blob_dev, At, ldat, Ct, ldct, M, bias, (int)act, true, stream, pl.xbuf_off != 0);
+    return launch_xcols(h, blob_dev, At, ldat, Ct, ldct, M, bias, (int)act, Rt, ldrt, true, stream, pl.xbuf_off != 0);
+}
+}  // namespace
+
+extern "C" int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, const void* At, int M, int ldat,
+                                  const void* bias, tw_act act, void* Ct, int ldct, void* workspace, size_t ws_bytes,
+                                  void* hip_stream) {
+    const int rc = check_gemm_t_args(blob_host, blob_dev, At, M, ldat, bias, act, Ct, ldct, workspace, ws_bytes);
+    if (rc || M == 0) return rc;
+    return run_gemm_t(blob_host, blob_dev, At, M, ldat, bias, act, nullptr, 0, Ct, ldct, workspace, ws_bytes, (hipStream_t)hip_stream);
+}
+
+extern "C" int tw_gemm_t_bias_act_add(const void* blob_host, const void* blob_dev, const void* At, int M, int ldat,
+                                      const void* bias, tw_act act, const void* Rt, int ldrt, void* Ct, int ldct, void* workspace,
+                                      size_t ws_bytes, void* hip_stream) {
+    const int rc = check_gemm_t_args(blob_host, blob_dev, At, M, ldat, bias, act, Ct, ldct, workspace, ws_bytes);
+    if (rc) return rc;
+    const TwHeader* h = (const TwHeader*)blob_host;
+    if (!Rt || ldrt < M || (Rt == Ct && ldrt != ldct)) return TW_ERR_ARG;
+    if ((ldrt & 7) != 0 || ((uintptr_t)Rt & 15) != 0) return TW_ERR_ALIGN;
+    if (adds_to_itself_twice(h, Rt, Ct)) return TW_ERR_UNSUPPORTED;
+    if (M == 0) return TW_OK;
+    return run_gemm_t(blob_host, blob_dev, At, M, ldat, bias, act, Rt, ldrt, Ct, ldct, workspace, ws_bytes, (hipStream_t)hip_stream);
 }
 
 // ---- the transposes at the two ends of a network that runs on the transposed boundary (Sec. VI) ----

@@ -69,3 +69,33 @@ def test_attention_refusals():
         assert attention(**kw) == want, kw
     assert attention(M=0, Q=None, K=None, V=None, O=None) == 0
     assert attention(n_seqs=0) == 0                              # no sequence, no row
+
+
+def test_add_refusals():
+    """The products that add a matrix: what they refuse beyond what the products without it do."""
+    import numpy as np
+    blob = tw.tw_pack(np.zeros((64, 96), np.uint16), np.ones((64, 96), np.uint8), 32, "f16")
+    tew = tw.tw_pack_tew(np.zeros((64, 96), np.uint16), np.r_[np.ones((63, 96), np.uint8), np.zeros((1, 96), np.uint8)] * (np.arange(96) > 0).astype(np.uint8),
+                         np.ones((64, 96), np.uint8), 32, "f16")
+    Q = 2 * P
+
+    def row(blob=blob, dev=P, A=P, M=4, lda=64, bias=None, act=0, R=P, ldr=96, C=Q, ldc=96, ws=P, n=256):
+        return tw._lib.tw_gemm_bias_act_add(blob.ctypes.data, dev, A, M, lda, bias, act, R, ldr, C, ldc, ws, n, None)
+
+    def col(blob=blob, dev=P, A=P, M=8, lda=8, bias=None, act=0, R=P, ldr=8, C=Q, ldc=8, ws=P, n=256):
+        return tw._lib.tw_gemm_t_bias_act_add(blob.ctypes.data, dev, A, M, lda, bias, act, R, ldr, C, ldc, ws, n, None)
+
+    def dense(A=P, lda=64, B=P, ldb=96, bias=None, act=0, R=P, ldr=96, C=Q, ldc=96, M=4, N=96, K=64, dt=0):
+        return tw._lib.tw_dense_gemm_bias_act_add(A, lda, B, ldb, bias, act, R, ldr, C, ldc, M, N, K, dt, None)
+
+    for kw, want in [(dict(R=None), ARG), (dict(ldr=95), ARG), (dict(R=P + 1), ALIGN), (dict(R=Q, ldr=104), ARG), (dict(ldr=1 << 23), UNSUPPORTED),
+                     (dict(A=None), ARG), (dict(C=None), ARG), (dict(act=3), ARG), (dict(bias=P + 1), ALIGN), (dict(lda=56), ARG), (dict(lda=68), ALIGN),
+                     (dict(ldc=95), ARG), (dict(M=-1), ARG), (dict(n=255), BUF), (dict(ws=P + 16), ALIGN), (dict(blob=tew, R=Q), UNSUPPORTED)]:
+        assert row(**kw) == want, kw
+    for kw, want in [(dict(R=None), ARG), (dict(ldr=7), ARG), (dict(ldr=12), ALIGN), (dict(R=P + 8), ALIGN), (dict(R=Q, ldr=16), ARG), (dict(A=None), ARG),
+                     (dict(act=-1), ARG), (dict(ldc=12), ALIGN), (dict(lda=0), ARG), (dict(n=0), BUF), (dict(blob=tew, R=Q), UNSUPPORTED)]:
+        assert col(**kw) == want, kw
+    for kw, want in [(dict(R=None), ARG), (dict(ldr=88), ARG), (dict(ldr=100), ALIGN), (dict(R=P + 8), ALIGN), (dict(R=Q, ldr=104), ARG), (dict(A=None), ARG),
+                     (dict(dt=2), ARG), (dict(act=9), ARG), (dict(K=0), ARG), (dict(M=-1), ARG)]:
+        assert dense(**kw) == want, kw
+    assert row(M=0) == 0 and col(M=0) == 0 and dense(M=0) == 0
