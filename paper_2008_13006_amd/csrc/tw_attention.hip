@@ -29,6 +29,7 @@ namespace {
 typedef unsigned short us;
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 constexpr int kRowsPerTile = 128, kKeys = 64;
+constexpr float kSlack = 8.f;
 constexpr unsigned kOut = 0x80000000u;      // an offset out of a buffer descriptor's range: fetches zeros
 
 struct AttnParams {
@@ -174,102 +175,136 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
     for (int f = 0; f < FB; ++f)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[f][r] = 0.f;
-    float m = -__builtin_inff(), l = 0.f;
+    // ref: what the exponents are taken from, at least the running maximum less kSlack; l: this lane's share of the sum of weights
+    float ref = -__builtin_inff(), l = 0.f;
 
-    auto work = [&](const unsigned char* buf, int k0, auto masked_tag) {
-        constexpr bool MASKED = decltype(masked_tag)::value;
-        const unsigned char* kb_ = buf;
-        const unsigned char* vb_ = buf + TILE;
+    // Where this lane's operands lie in a tile.  Scores: row (key) 32 b + l32, piece (2 ks + h) ^ fk; values: rows 16 st + 4 h + j / 4 (+ 8), piece
+    // (4 f + ..) ^ fv.  The swizzles repeat every 16 (8) rows, so blocks and steps are constant offsets, and ks and f flip bits.
+    const int j = lane & 15;
+    const unsigned ka = (unsigned)(l32 * ROW + ((h ^ fk(l32)) << 4));
+    const int vr = 4 * h + (j >> 2);
+    const unsigned va = (unsigned)(TILE + vr * ROW + (((2 * ((lane >> 4) & 1) + ((j & 3) >> 1)) ^ fv(vr)) << 4) + (j & 1) * 8);
+    auto value_operand = [&](const unsigned char* buf, int st, int f) {
+        const unsigned char* at = buf + (va ^ (unsigned)(f << 6)) + 16 * st * ROW;
+        const i16x4 a = read_tr(at), c = read_tr(at + 8 * ROW);
+        return tw_u16x8{(us)a[0], (us)a[1], (us)a[2], (us)a[3], (us)c[0], (us)c[1], (us)c[2], (us)c[3]};
+    };
+
+    // a scale of zero is taken into the scores: the mark of a key that is not seen, -inf, must not meet it
+    const bool flat = p.scale2 == 0.f;
+    const float scale2 = flat ? 1.f : p.scale2;
+
+    auto work = [&](const unsigned char* buf, int k0) {
+        const bool whole = k0 >= inner0 && k0 + kKeys <= inner1;          // every row sees every key (wave-uniform)
         tw_f32x16 s[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int kr = 32 * b + l32;
-                const tw_u16x8 a = *(const tw_u16x8*)(kb_ + kr * ROW + (((2 * ks + h) ^ fk(kr)) << 4));
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const tw_u16x8 a = *(const tw_u16x8*)(buf + (ka ^ (unsigned)(ks << 5)) + 32 * b * ROW);
                 s[b] = tw_mfma<DT>(a, q[ks], s[b]);
             }
+        if (flat) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] *= 0.f;
         }
-        float top = -__builtin_inff();
+        bool odd = false;                                    // (wave-uniform) values that are not finite beside keys that some row does not see
+        if (!whole) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[b][r] *= p.scale2;
-                if constexpr (MASKED) {
+                for (int r = 0; r < 16; ++r) {
                     const int key = k0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3);
                     if ((unsigned)(key - lo) >= (unsigned)(hi - lo)) s[b][r] = -__builtin_inff();
                 }
-                top = __builtin_fmaxf(top, s[b][r]);
-            }
-        top = __builtin_fmaxf(top, __shfl_xor(top, 32));
-        const float m_new = __builtin_fmaxf(m, top);
-        const float ref = m_new == -__builtin_inff() ? 0.f : m_new;     // (no key yet, or only scores of -inf: all weights 0)
-        const float fade = __builtin_amdgcn_exp2f(m - ref);
-        m = m_new;
-        l *= fade;
+            constexpr us kInf = DT == TW_F16 ? 0x7C00 : 0x7F80;
+            tw_u16x8 most{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-        for (int f = 0; f < FB; ++f)
+            for (int st = 0; st < 4; ++st)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[f][r] *= fade;
+                for (int f = 0; f < FB; ++f) most = __builtin_elementwise_max(most, value_operand(buf, st, f) & (us)0x7FFF);
+            bool mine = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mine |= most[e] >= kInf;
+            odd = __any(mine);
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[b][r]);
+        top = __builtin_fmaxf(top, __shfl_xor(top, 32)) * scale2;
+        // The exponents' reference moves only when some row's maximum has grown by more than kSlack powers of two: the weights stay below
+        // 2^kSlack, which 16 bits hold as precisely, and most tiles scale nothing.
+        if (__any(top > ref + kSlack)) {
+            const float next = __builtin_fmaxf(ref, top);
+            const float from = ref == -__builtin_inff() ? next : ref;     // (nothing summed yet; -inf twice: no key seen)
+            const float fade = __builtin_amdgcn_exp2f(ref == next ? 0.f : from - next);
+            ref = next;
+            l *= fade;
+#pragma unroll
+            for (int f = 0; f < FB; ++f)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[f][r] *= fade;
+        }
+        const float base = ref == -__builtin_inff() ? 0.f : ref;          // (no key yet, or only scores of -inf: all weights 0)
         tw_u16x8 w[4];                                       // weights: operand of contraction step 2 b + r / 8
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float e = __builtin_amdgcn_exp2f(s[b][r] - ref);
-                l += e;
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], scale2, -base));
+                sum[r & 3] += e;
                 w[2 * b + (r >> 3)][r & 7] = tw_cvt<DT>(e);
             }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         // O^T += V^T P^T.  Slots 8 h + 0..3 and 8 h + 4..7 of step st are the keys 16 st + 4 h + 0..3 and 16 st + 8 + 4 h + 0..3
-        bool odd = false;                                    // a value that is not finite in a tile that some row does not see in full
-        const int j = lane & 15;
+        if (!odd) {
 #pragma unroll
-        for (int st = 0; st < 4; ++st)
+            for (int st = 0; st < 4; ++st)
 #pragma unroll
-            for (int f = 0; f < FB; ++f) {
-                const int ra = 16 * st + 4 * h + (j >> 2), rb = ra + 8;
-                const int piece = 4 * f + 2 * ((lane >> 4) & 1) + ((j & 3) >> 1);
-                const i16x4 a = read_tr(vb_ + ra * ROW + ((piece ^ fv(ra)) << 4) + (j & 1) * 8);
-                const i16x4 c = read_tr(vb_ + rb * ROW + ((piece ^ fv(rb)) << 4) + (j & 1) * 8);
-                tw_u16x8 x{(us)a[0], (us)a[1], (us)a[2], (us)a[3], (us)c[0], (us)c[1], (us)c[2], (us)c[3]};
-                if constexpr (MASKED) {
-                    constexpr us kInf = DT == TW_F16 ? 0x7C00 : 0x7F80;
+                for (int f = 0; f < FB; ++f) o[f] = tw_mfma<DT>(value_operand(buf, st, f), w[st], o[f]);
+        } else {                                             // rare: a weight of zero must not meet them; they reach the rows that see their key
+            constexpr us kInf = DT == TW_F16 ? 0x7C00 : 0x7F80;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if ((x[e] & 0x7FFF) >= kInf) { x[e] = 0; odd = true; }   // a weight of zero must not meet it
+            for (int st = 0; st < 4; ++st)
+#pragma unroll
+                for (int f = 0; f < FB; ++f) {
+                    tw_u16x8 x = value_operand(buf, st, f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = (x[e] & 0x7FFF) >= kInf ? (us)0 : x[e];
+                    o[f] = tw_mfma<DT>(x, w[st], o[f]);
                 }
-                o[f] = tw_mfma<DT>(x, w[st], o[f]);
-            }
-        if constexpr (MASKED) {
-            if (__any(odd)) {                                // rare: such values reach the rows that see their key, one by one
-                for (int kk = 0; kk < kKeys; ++kk) {
-                    const bool sees = (unsigned)(k0 + kk - lo) < (unsigned)(hi - lo);
+            for (int kk = 0; kk < kKeys; ++kk) {
+                const bool sees = (unsigned)(k0 + kk - lo) < (unsigned)(hi - lo);
 #pragma unroll
-                    for (int f = 0; f < FB; ++f)
+                for (int f = 0; f < FB; ++f)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int c = 32 * f + 8 * (r >> 2) + 4 * h + (r & 3);
-                            const float x = tw_to_f32<DT>(*(const us*)(vb_ + kk * ROW + (((c >> 3) ^ fv(kk)) << 4) + (c & 7) * 2));
-                            if (sees && !(__builtin_fabsf(x) < __builtin_inff())) o[f][r] += x;
-                        }
-                }
+                    for (int r = 0; r < 16; ++r) {
+                        const int c = 32 * f + 8 * (r >> 2) + 4 * h + (r & 3);
+                        const float x = tw_to_f32<DT>(*(const us*)(buf + TILE + kk * ROW + (((c >> 3) ^ fv(kk)) << 4) + (c & 7) * 2));
+                        if (sees && !(__builtin_fabsf(x) < __builtin_inff())) o[f][r] += x;
+                    }
             }
         }
     };
 
     issue(k_begin, 0);
-    int buf = 0;
-    for (int k0 = k_begin; k0 < k_end; k0 += kKeys, buf ^= 1) {
+    auto turn = [&](int k0, int buf) {                       // (buf: a constant)
         tw_lds_wait<0>();                                    // the tile has landed, and nobody reads the other buffer any more
         if (k0 + kKeys < k_end) issue(k0 + kKeys, buf ^ 1);
-        if (k0 < last && k0 + kKeys > first) {               // (wave-uniform)
-            const unsigned char* b = smem + buf * (2 * TILE);
-            if (k0 >= inner0 && k0 + kKeys <= inner1) work(b, k0, std::integral_constant<bool, false>{});
-            else work(b, k0, std::integral_constant<bool, true>{});
-        }
+        if (k0 < last && k0 + kKeys > first) work(smem + buf * (2 * TILE), k0);   // (wave-uniform)
+    };
+    for (int k0 = k_begin; k0 < k_end; k0 += 2 * kKeys) {
+        turn(k0, 0);
+        if (k0 + kKeys < k_end) turn(k0 + kKeys, 1);
     }
     l += __shfl_xor(l, 32);
     const float inv = 1.f / l;
