@@ -50,6 +50,12 @@ __device__ __forceinline__ tw_u32x4 descriptor(const us* base) {
     const uint64_t a = (uint64_t)base;
     return tw_u32x4{(unsigned)uni((int)(unsigned)a), (unsigned)uni((int)(unsigned)(a >> 32)) & 0xFFFFu, kOut, 0x00020000u};
 }
+// The larger of a value and that of the other lane half (lane ^ 32).
+__device__ __forceinline__ float max_halves(float x) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned low = both[0], high = both[1];            // (copies: the builtin cast of a vector's element takes the first one)
+    return __builtin_fmaxf(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
+}
 __device__ __forceinline__ i16x4 read_tr(const unsigned char* a) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)a);
 }
@@ -157,17 +163,13 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
     const unsigned ldk2 = 2u * (unsigned)p.ldk, ldv2 = 2u * (unsigned)p.ldv;
     constexpr int RPR = 1024 / ROW;                          // rows per request
     const int frow = lane / PIECES, fslot = lane % PIECES;
-    auto issue = [&](int k0, int buf) {                      // the tile of keys k0 ..
-        const tw_u32x4 dk = descriptor(kbase + (long)k0 * p.ldk), dv = descriptor(vbase + (long)k0 * p.ldv);
-        const unsigned dst = lds0 + (unsigned)buf * (2 * TILE);
-        const int left = p.M - k0;
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int r = (wave * LOADS + i) * RPR + frow;
-            const int pk = fslot ^ fk(r), pv = fslot ^ fv(r);
-            tw_load_lds<false>(dk, r < left && 8 * pk < p.d ? (unsigned)r * ldk2 + pk * 16 : kOut, dst + (wave * LOADS + i) * 1024u);
-            tw_load_lds<false>(dv, r < left && 8 * pv < p.d ? (unsigned)r * ldv2 + pv * 16 : kOut, dst + TILE + (wave * LOADS + i) * 1024u);
-        }
+    // Request i of the tile of keys k0 .., the first LOADS of K, the others of V.  Rows behind the last key are out of range.
+    auto request = [&](int k0, int buf, int i) __attribute__((always_inline)) {
+        const bool of_v = i >= LOADS;
+        const int n = of_v ? i - LOADS : i, r = (wave * LOADS + n) * RPR + frow, pc = fslot ^ (of_v ? fv(r) : fk(r));
+        const us* base = of_v ? vbase + (long)k0 * p.ldv : kbase + (long)k0 * p.ldk;
+        tw_load_lds<false>(descriptor(base), r < k_end - k0 && 8 * pc < p.d ? (unsigned)r * (of_v ? ldv2 : ldk2) + pc * 16 : kOut,
+                           lds0 + (unsigned)buf * (2 * TILE) + (of_v ? TILE : 0) + (wave * LOADS + n) * 1024u);
     };
 
     tw_f32x16 o[FB];
@@ -184,37 +186,46 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
     const unsigned ka = (unsigned)(l32 * ROW + ((h ^ fk(l32)) << 4));
     const int vr = 4 * h + (j >> 2);
     const unsigned va = (unsigned)(TILE + vr * ROW + (((2 * ((lane >> 4) & 1) + ((j & 3) >> 1)) ^ fv(vr)) << 4) + (j & 1) * 8);
-    auto value_operand = [&](const unsigned char* buf, int st, int f) {
+    auto value_operand = [&](const unsigned char* buf, int st, int f) __attribute__((always_inline)) {
         const unsigned char* at = buf + (va ^ (unsigned)(f << 6)) + 16 * st * ROW;
-        const i16x4 a = read_tr(at), c = read_tr(at + 8 * ROW);
-        return tw_u16x8{(us)a[0], (us)a[1], (us)a[2], (us)a[3], (us)c[0], (us)c[1], (us)c[2], (us)c[3]};
+        return __builtin_bit_cast(tw_u16x8, __builtin_shufflevector(read_tr(at), read_tr(at + 8 * ROW), 0, 1, 2, 3, 4, 5, 6, 7));
     };
-
     // a scale of zero is taken into the scores: the mark of a key that is not seen, -inf, must not meet it
     const bool flat = p.scale2 == 0.f;
     const float scale2 = flat ? 1.f : p.scale2;
+    constexpr us kInf = DT == TW_F16 ? 0x7C00 : 0x7F80;
+    bool odd = false;                                        // values that are not finite lie beside keys that some row does not see
+    constexpr int kAhead = 4;                                // operands are read that many products ahead
 
-    auto work = [&](const unsigned char* buf, int k0) {
+    // The tile of keys k0 .. in `buf`; next(i) makes request i for the tile after it.
+    auto work = [&](const unsigned char* buf, int k0, auto next) __attribute__((always_inline)) {
         const bool whole = k0 >= inner0 && k0 + kKeys <= inner1;          // every row sees every key (wave-uniform)
         tw_f32x16 s[2];
+        tw_u16x8 x[kAhead];
+        auto key_operand = [&](int n) __attribute__((always_inline)) {
+            return *(const tw_u16x8*)(buf + (ka ^ (unsigned)((n >> 1) << 5)) + 32 * (n & 1) * ROW);
+        };
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+        for (int n = 0; n < kAhead && n < 2 * KS; ++n) x[n] = key_operand(n);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const tw_u16x8 a = *(const tw_u16x8*)(buf + (ka ^ (unsigned)(ks << 5)) + 32 * b * ROW);
-                s[b] = tw_mfma<DT>(a, q[ks], s[b]);
-            }
+        for (int n = 0; n < 2 * KS; ++n) {
+            __builtin_amdgcn_sched_barrier(0);
+            s[n & 1] = tw_mfma<DT>(x[n % kAhead], q[n >> 1], s[n & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (n + kAhead < 2 * KS) x[n % kAhead] = key_operand(n + kAhead);
+        }
         if (flat) {
+            float zero = 0.f;
+            asm volatile("" : "+v"(zero));                   // (or the products are made ahead of the branch, for every tile)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[b][r] *= 0.f;
+                for (int r = 0; r < 16; ++r) s[b][r] *= zero;
         }
-        bool odd = false;                                    // (wave-uniform) values that are not finite beside keys that some row does not see
         if (!whole) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -223,30 +234,31 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
                     const int key = k0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3);
                     if ((unsigned)(key - lo) >= (unsigned)(hi - lo)) s[b][r] = -__builtin_inff();
                 }
-            constexpr us kInf = DT == TW_F16 ? 0x7C00 : 0x7F80;
+            // a weight of zero must not meet a value that is not finite: see the end
             tw_u16x8 most{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
             for (int st = 0; st < 4; ++st)
 #pragma unroll
-                for (int f = 0; f < FB; ++f) most = __builtin_elementwise_max(most, value_operand(buf, st, f) & (us)0x7FFF);
-            bool mine = false;
+                for (int f = 0; f < FB; ++f)
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(tw_u16x8, __builtin_bit_cast(tw_u32x4, value_operand(buf, st, f)) & 0x7FFF7FFFu));
+            bool any = false;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) mine |= most[e] >= kInf;
-            odd = __any(mine);
+            for (int e = 0; e < 8; ++e) any |= most[e] >= kInf;
+            odd |= __any(any) != 0;
         }
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[b][r]);
-        top = __builtin_fmaxf(top, __shfl_xor(top, 32)) * scale2;
+        top = max_halves(top) * scale2;
         // The exponents' reference moves only when some row's maximum has grown by more than kSlack powers of two: the weights stay below
         // 2^kSlack, which 16 bits hold as precisely, and most tiles scale nothing.
         if (__any(top > ref + kSlack)) {
-            const float next = __builtin_fmaxf(ref, top);
-            const float from = ref == -__builtin_inff() ? next : ref;     // (nothing summed yet; -inf twice: no key seen)
-            const float fade = __builtin_amdgcn_exp2f(ref == next ? 0.f : from - next);
-            ref = next;
+            const float next_ref = __builtin_fmaxf(ref, top);
+            const float from = ref == -__builtin_inff() ? next_ref : ref;     // (nothing summed yet; -inf twice: no key seen)
+            const float fade = __builtin_amdgcn_exp2f(ref == next_ref ? 0.f : from - next_ref);
+            ref = next_ref;
             l *= fade;
 #pragma unroll
             for (int f = 0; f < FB; ++f)
@@ -256,57 +268,86 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
         const float base = ref == -__builtin_inff() ? 0.f : ref;          // (no key yet, or only scores of -inf: all weights 0)
         tw_u16x8 w[4];                                       // weights: operand of contraction step 2 b + r / 8
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        // A request for the next tile, then its share of the exponentials: a compute unit takes 64 bytes of requests a clock, and a wave that makes
+        // all of its own at once waits for that.
+        constexpr int kShare = 32 / (2 * LOADS);
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], scale2, -base));
-                sum[r & 3] += e;
-                w[2 * b + (r >> 3)][r & 7] = tw_cvt<DT>(e);
+        for (int i = 0; i < 32; ++i) {
+            const int b = i >> 4, r = i & 15;
+            if (i % kShare == 0) {
+                __builtin_amdgcn_sched_barrier(0);
+                next(i / kShare);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], scale2, -base));
+            sum[r & 3] += e;
+            w[2 * b + (r >> 3)][r & 7] = tw_cvt<DT>(e);
+        }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         // O^T += V^T P^T.  Slots 8 h + 0..3 and 8 h + 4..7 of step st are the keys 16 st + 4 h + 0..3 and 16 st + 8 + 4 h + 0..3
-        if (!odd) {
 #pragma unroll
-            for (int st = 0; st < 4; ++st)
+        for (int n = 0; n < kAhead; ++n) x[n] = value_operand(buf, n / FB, n % FB);
 #pragma unroll
-                for (int f = 0; f < FB; ++f) o[f] = tw_mfma<DT>(value_operand(buf, st, f), w[st], o[f]);
-        } else {                                             // rare: a weight of zero must not meet them; they reach the rows that see their key
-            constexpr us kInf = DT == TW_F16 ? 0x7C00 : 0x7F80;
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int f = 0; f < FB; ++f) {
-                    tw_u16x8 x = value_operand(buf, st, f);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = (x[e] & 0x7FFF) >= kInf ? (us)0 : x[e];
-                    o[f] = tw_mfma<DT>(x, w[st], o[f]);
-                }
-            for (int kk = 0; kk < kKeys; ++kk) {
-                const bool sees = (unsigned)(k0 + kk - lo) < (unsigned)(hi - lo);
-#pragma unroll
-                for (int f = 0; f < FB; ++f)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int c = 32 * f + 8 * (r >> 2) + 4 * h + (r & 3);
-                        const float x = tw_to_f32<DT>(*(const us*)(buf + TILE + kk * ROW + (((c >> 3) ^ fv(kk)) << 4) + (c & 7) * 2));
-                        if (sees && !(__builtin_fabsf(x) < __builtin_inff())) o[f][r] += x;
-                    }
-            }
+        for (int n = 0; n < 4 * FB; ++n) {
+            __builtin_amdgcn_sched_barrier(0);
+            o[n % FB] = tw_mfma<DT>(x[n % kAhead], w[n / FB], o[n % FB]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (n + kAhead < 4 * FB) x[n % kAhead] = value_operand(buf, (n + kAhead) / FB, (n + kAhead) % FB);
         }
     };
 
-    issue(k_begin, 0);
-    auto turn = [&](int k0, int buf) {                       // (buf: a constant)
+#pragma unroll
+    for (int i = 0; i < 2 * LOADS; ++i) request(k_begin, 0, i);
+    auto turn = [&](int k0, int buf) __attribute__((always_inline)) {     // (buf: a constant)
         tw_lds_wait<0>();                                    // the tile has landed, and nobody reads the other buffer any more
-        if (k0 + kKeys < k_end) issue(k0 + kKeys, buf ^ 1);
-        if (k0 < last && k0 + kKeys > first) work(smem + buf * (2 * TILE), k0);   // (wave-uniform)
+        // (behind the last tile the requests are out of range)
+        auto next = [&](int i) __attribute__((always_inline)) { request(k0 + kKeys, buf ^ 1, i); };
+        if (k0 < last && k0 + kKeys > first) {               // (wave-uniform)
+            work(smem + buf * (2 * TILE), k0, next);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * LOADS; ++i) next(i);
+        }
     };
     for (int k0 = k_begin; k0 < k_end; k0 += 2 * kKeys) {
         turn(k0, 0);
         if (k0 + kKeys < k_end) turn(k0 + kKeys, 1);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // nothing on its way into LDS any more
     l += __shfl_xor(l, 32);
+            // Rare: a value that is not finite, beside keys that some row of the wave does not see, has met a weight of zero there.  The sums with V
+            // are made again, key by key, each row's own keys only (maximum and sum of the weights do not depend on V).
+            if (odd) {
+    #pragma unroll
+                for (int f = 0; f < FB; ++f)
+    #pragma unroll
+                    for (int r = 0; r < 16; ++r) o[f][r] = 0.f;
+    #pragma unroll 1
+                for (int key = first; key < last; ++key) {
+                    const us* krow = p.k + (long)key * p.ldk + (long)kvh * p.d;
+                    const us* vrow = p.v + (long)key * p.ldv + (long)kvh * p.d;
+                    float x = 0.f;
+    #pragma unroll
+                    for (int ks = 0; ks < KS; ++ks)
+                        if (16 * ks + 8 * h < p.d) {
+                            const tw_u16x8 kv = *(const tw_u16x8*)(krow + 16 * ks + 8 * h);
+    #pragma unroll
+                            for (int e = 0; e < 8; ++e) x = __builtin_fmaf(tw_to_f32<DT>(kv[e]), tw_to_f32<DT>(q[ks][e]), x);
+                        }
+                    x += __shfl_xor(x, 32);
+                    if (flat) x *= 0.f;
+                    const float e = tw_to_f32<DT>(tw_cvt<DT>(__builtin_amdgcn_exp2f(__builtin_fmaf(x, scale2, ref == -__builtin_inff() ? 0.f : -ref))));
+                    if ((unsigned)(key - lo) >= (unsigned)(hi - lo)) continue;
+    #pragma unroll
+                    for (int f = 0; f < FB; ++f)
+    #pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int c = 32 * f + 8 * (r >> 2) + 4 * h + (r & 3);
+                            const float v = c < p.d ? tw_to_f32<DT>(vrow[c]) : 0.f;
+                            o[f][r] += __builtin_fabsf(v) < __builtin_inff() ? e * v : v;
+                        }
+                }
+            }
     const float inv = 1.f / l;
     __syncthreads();                                         // the staging areas of the results lie over the tiles
     unsigned char* stage = smem + wave * (32 * OPITCH);
