@@ -309,7 +309,7 @@ int tw_dense_gemm_bias_act_add(const void* A, int lda, const void* B, int ldb, c
  * Sums are fp32, the variance is taken about the mean, Y is rounded once.  Non-finite values stay within their row.
  * M >= 0 (M = 0 enqueues nothing).  One kernel, no workspace; it can be recorded into a HIP graph.
  * Errors: TW_ERR_ARG (null X or Y, negative M, N <= 0, pitch too small, unknown dt, eps), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED
- * (N above 2^24 - 256; tw_layernorm_t also M above 2^28), TW_ERR_HIP. */
+ * (N above 2^24 - 256; tw_layernorm_t also M above 2^27 - 64), TW_ERR_HIP. */
 int tw_layernorm(const void* X, int ldx, int M, int N, const void* gamma, const void* beta, float eps, void* Y, int ldy,
                  float* mean, float* rstd, tw_dtype dt, void* hip_stream);
 

@@ -28,6 +28,7 @@ struct LnParams {
     long ldx, ldy;
     int M, N;
     float eps;
+    int stream;                 // rows of y start on 128-byte boundaries: whole lines go out as streaming stores
 };
 
 // Sum over groups of TPR consecutive lanes, the same bits in every lane of the group.
@@ -189,16 +190,17 @@ __device__ __forceinline__ void forget(tw_u32x4 (&w)[PER]) {
     for (int i = 0; i < PER; ++i) asm volatile("" : "+v"(w[i]));
 }
 
-// Transposed boundary: features are rows, tokens columns.  A workgroup takes 64 tokens (a line of every row), a lane the 16-byte piece
-// lane % 8 of row lane / 8 + 8 * wave + 8 * WAVES * i, PER of them, which wait in registers as they were read.  A token's sums meet across
-// the eight lanes of a wave that hold its piece and, through LDS, across the waves.
+constexpr int kTPieces = 8, PCS = kTPieces;
+// Transposed boundary: features are rows, tokens columns.  A workgroup takes 8 * PCS tokens, a lane the 16-byte piece lane % PCS of the rows
+// lane / PCS + 64 / PCS * wave + 64 / PCS * WAVES * i, PER of them, which wait in registers as they were read.  A token's sums meet across
+// the lanes of a wave that hold its piece and, through LDS, across the waves.
 template <int DT, int WAVES, int PER>
 __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
-    constexpr int kRows = 8 * WAVES;
-    __shared__ float red[2][WAVES][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pc = lane & 7;
-    const long m0 = (long)blockIdx.x * 64 + 8 * pc;
-    const int n0 = 8 * wave + (lane >> 3);
+    constexpr int kRows = 64 / PCS * WAVES;
+    __shared__ float red[2][WAVES][8 * PCS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pc = lane % PCS;
+    const long m0 = (long)blockIdx.x * (8 * PCS) + 8 * pc;
+    const int n0 = 64 / PCS * wave + lane / PCS;
     const bool here = m0 < p.M;
     const float inv_n = 1.f / (float)p.N;
     tw_u32x4 w[PER];
@@ -210,11 +212,10 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
     auto across = [&](float (&s)[8], int turn) {             // sums of the eight tokens over all rows
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            s[e] += __shfl_xor(s[e], 8);
-            s[e] += __shfl_xor(s[e], 16);
-            s[e] += __shfl_xor(s[e], 32);
+#pragma unroll
+            for (int k = PCS; k < 64; k <<= 1) s[e] += __shfl_xor(s[e], k);
         }
-        if (lane < 8) {
+        if (lane < PCS) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) red[turn][wave][8 * pc + e] = s[e];
         }
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) rstd[e] = 1.f / sqrtf(rstd[e] * inv_n + p.eps);
     if (!here) return;
-    if (threadIdx.x < 8) {
+    if (threadIdx.x < PCS) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (m0 + e < p.M) {
@@ -267,16 +268,107 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
     }
     const int left = p.M - m0 < 8 ? (int)(p.M - m0) : 8;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int n = n0 + kRows * i;
-        if (n >= p.N) continue;
+    for (int i0 = 0; i0 < PER; i0 += 4) {                    // (four rows at a time: unpacked all at once they would not fit)
+        float g[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4 && i0 + i < PER; ++i) {
+            const int n = n0 + kRows * (i0 + i), at = n < p.N ? n : p.N - 1;
+            g[i] = p.gamma ? tw_to_f32<DT>(p.gamma[at]) : 1.f;
+            b[i] = p.beta ? tw_to_f32<DT>(p.beta[at]) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4 && i0 + i < PER; ++i) {
+            const int n = n0 + kRows * (i0 + i);
+            float f[8];
+            unpack8<DT>(w[i0 + i], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf((f[e] - mean[e]) * rstd[e], g[i], b[i]);
+            if (n >= p.N) continue;
+            if (p.stream && left == 8) tw_store16_stream(p.y + (long)n * p.ldy + m0, pack8<DT>(f));
+            else put8<true>(tw_opaque(p.y) + (long)n * p.ldy + m0, left, pack8<DT>(f));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// The same for rows that do not fit the registers: they are read three times (from the caches after the first), four requests of a lane at a time.
+template <int DT>
+__global__ __launch_bounds__(1024) void tw_ln_t_loop_kernel(const LnParams p) {
+    constexpr int WAVES = 16, kRows = 64 / PCS * WAVES;
+    __shared__ float red[2][WAVES][8 * PCS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pc = lane % PCS;
+    const long m0 = (long)blockIdx.x * (8 * PCS) + 8 * pc;
+    const int n0 = 64 / PCS * wave + lane / PCS;
+    const bool here = m0 < p.M;
+    const float inv_n = 1.f / (float)p.N;
+    auto across = [&](float (&s)[8], int turn) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+#pragma unroll
+            for (int k = PCS; k < 64; k <<= 1) s[e] += __shfl_xor(s[e], k);
+        }
+        if (lane < PCS) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) red[turn][wave][8 * pc + e] = s[e];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) s[e] += red[turn][k][8 * pc + e];
+        }
+    };
+    auto rows = [&](auto use) {                              // use(row, its piece) for this lane's rows
+        for (int n = n0; n < p.N; n += 4 * kRows) {
+            tw_u32x4 w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = tw_u32x4{0u, 0u, 0u, 0u};
+                if (here && n + i * kRows < p.N) w[i] = *(const tw_u32x4*)(p.x + (long)(n + i * kRows) * p.ldx + m0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (n + i * kRows < p.N) use(n + i * kRows, w[i]);
+        }
+    };
+    float mean[8] = {}, rstd[8] = {};
+    rows([&](int, tw_u32x4 w) {
+        float f[8];
+        unpack8<DT>(w, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mean[e] += f[e];
+    });
+    across(mean, 0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mean[e] *= inv_n;
+    rows([&](int, tw_u32x4 w) {
+        float f[8];
+        unpack8<DT>(w, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rstd[e] = __builtin_fmaf(f[e] - mean[e], f[e] - mean[e], rstd[e]);
+    });
+    across(rstd, 1);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rstd[e] = 1.f / sqrtf(rstd[e] * inv_n + p.eps);
+    if (!here) return;
+    if (threadIdx.x < PCS) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (m0 + e < p.M) {
+                if (p.mean) p.mean[m0 + e] = mean[e];
+                if (p.rstd) p.rstd[m0 + e] = rstd[e];
+            }
+    }
+    const int left = p.M - m0 < 8 ? (int)(p.M - m0) : 8;
+    rows([&](int n, tw_u32x4 w) {
         const float g = p.gamma ? tw_to_f32<DT>(p.gamma[n]) : 1.f, b = p.beta ? tw_to_f32<DT>(p.beta[n]) : 0.f;
         float f[8];
-        unpack8<DT>(w[i], f);
+        unpack8<DT>(w, f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf((f[e] - mean[e]) * rstd[e], g, b);
         put8<true>(p.y + (long)n * p.ldy + m0, left, pack8<DT>(f));
-    }
+    });
 }
 
 // Transposed boundary, any pitch, alignment and N: a lane per token, the rows dealt out to the waves, read three times.
@@ -487,26 +579,40 @@ __global__ __launch_bounds__(256) void tw_ln_grad_cols_kernel(const LnGradParams
     p.part_beta[(long)blockIdx.x * p.N + c] = sb;
 }
 
-// dst[n] = sum over the parts, 64 columns to a workgroup, every fourth part to a wave, then the four waves' sums in order.
-// blockIdx.y: dgamma or dbeta.
-__global__ __launch_bounds__(256) void tw_ln_grad_sum_kernel(const float* part_gamma, const float* part_beta, int n_parts, int N,
-                                                             float* dgamma, float* dbeta) {
-    __shared__ float red[4][64];
+// dst[n] = sum over the parts: 32 columns to a workgroup, every 32nd part to half a wave, eight requests on their way, then the halves' sums in
+// order.  blockIdx.y: dgamma or dbeta.  (64 columns and four waves, a request at a time: 32 us for 512 parts of 768 columns.)
+__global__ __launch_bounds__(1024) void tw_ln_grad_sum_kernel(const float* part_gamma, const float* part_beta, int n_parts, int N,
+                                                              float* dgamma, float* dbeta) {
+    __shared__ float red[32][32];
     const float* src = blockIdx.y ? part_beta : part_gamma;
     float* dst = blockIdx.y ? dbeta : dgamma;
-    if (!dst) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long c = (long)blockIdx.x * 64 + lane;
+    if (!dst) return;                                        // (uniform)
+    const int col = threadIdx.x & 31, half = threadIdx.x >> 5;
+    const long c = (long)blockIdx.x * 32 + col;
     float s = 0.f;
-    if (c < N)
-        for (int k = wave; k < n_parts; k += 4) s += src[(long)k * N + c];
-    red[wave][lane] = s;
+    if (c < N) {
+        int k = half;
+        for (; k + 7 * 32 < n_parts; k += 8 * 32) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = src[(long)(k + 32 * i) * N + c];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i];
+        }
+        for (; k < n_parts; k += 32) s += src[(long)k * N + c];
+    }
+    red[half][col] = s;
     __syncthreads();
-    if (wave == 0 && c < N) dst[c] = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    if (half == 0 && c < N) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t += red[i][col];
+        dst[c] = t;
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ host
-constexpr int kMaxFeatures = (1 << 24) - 256;   // (the grids of the backward pass' column kernels)
+constexpr int kMaxFeatures = (1 << 24) - 256;   // (65535 workgroups of 256 columns; half a million of 1024 threads)
 
 // Threads of a row and 16-byte pieces of a thread for N features; false: the row does not fit the registers of 256 threads.
 bool row_shape(int N, int& tpr, int& per) {
@@ -545,7 +651,8 @@ const void* pick_t(int N) {
     if (N <= 256) return (const void*)tw_ln_t_kernel<DT, 8, 4>;
     if (N <= 512) return (const void*)tw_ln_t_kernel<DT, 8, 8>;
     if (N <= 768) return (const void*)tw_ln_t_kernel<DT, 8, 12>;
-    return N <= 1024 ? (const void*)tw_ln_t_kernel<DT, 8, 16> : (const void*)tw_ln_t_kernel<DT, 16, 16>;
+    if (N <= 1024) return (const void*)tw_ln_t_kernel<DT, 8, 16>;
+    return N <= 2048 ? (const void*)tw_ln_t_kernel<DT, 8, 32> : (const void*)tw_ln_t_loop_kernel<DT>;
 }
 
 bool odd(const void* q) { return ((uintptr_t)q & 1) != 0; }
@@ -580,7 +687,7 @@ extern "C" int tw_layernorm(const void* X, int ldx, int M, int N, const void* ga
     const int rc = check_forward(X, ldx, M, N, gamma, beta, eps, Y, ldy, mean, rstd, dt, N);
     if (rc) return rc;
     if (M == 0) return TW_OK;
-    LnParams p{(const us*)X, (const us*)gamma, (const us*)beta, (us*)Y, mean, rstd, ldx, ldy, M, N, eps};
+    LnParams p{(const us*)X, (const us*)gamma, (const us*)beta, (us*)Y, mean, rstd, ldx, ldy, M, N, eps, 0};
     int tpr = 0, per = 0;
     const bool vec = vec16(X) && vec16(Y) && vec16(gamma) && vec16(beta) && (ldx & 7) == 0 && (ldy & 7) == 0;
     if (vec && row_shape(N, tpr, per)) {
@@ -596,12 +703,12 @@ extern "C" int tw_layernorm_t(const void* Xt, int ldxt, int M, int N, const void
     const int rc = check_forward(Xt, ldxt, M, N, gamma, beta, eps, Yt, ldyt, mean, rstd, dt, M);
     if (rc) return rc;
     if (M == 0) return TW_OK;
-    LnParams p{(const us*)Xt, (const us*)gamma, (const us*)beta, (us*)Yt, mean, rstd, ldxt, ldyt, M, N, eps};
-    if (M > (1 << 28)) return TW_ERR_UNSUPPORTED;            // (a workgroup of up to 1024 threads per 64 tokens)
+    LnParams p{(const us*)Xt, (const us*)gamma, (const us*)beta, (us*)Yt, mean, rstd, ldxt, ldyt, M, N, eps,
+               ((uintptr_t)Yt & 127) == 0 && (ldyt & 63) == 0};
+    if (M > (1 << 27) - 64) return TW_ERR_UNSUPPORTED;       // (a workgroup of up to 1024 threads per 32 tokens)
+    if (vec16(Xt) && vec16(Yt) && (ldxt & 7) == 0 && (ldyt & 7) == 0)
+        return launch(dt == TW_F16 ? pick_t<TW_F16>(N) : pick_t<TW_BF16>(N), dim3((unsigned)((M + 8L * kTPieces - 1) / (8 * kTPieces))), dim3(N <= 2048 ? 512 : 1024), &p, 0, hip_stream);
     const dim3 grid((unsigned)((M + 63L) / 64));
-    const bool vec = vec16(Xt) && vec16(Yt) && (ldxt & 7) == 0 && (ldyt & 7) == 0;
-    if (vec && N <= 2048)
-        return launch(dt == TW_F16 ? pick_t<TW_F16>(N) : pick_t<TW_BF16>(N), grid, dim3(N <= 1024 ? 512 : 1024), &p, 0, hip_stream);
     const void* fn = dt == TW_F16 ? (const void*)tw_ln_t_any_kernel<TW_F16> : (const void*)tw_ln_t_any_kernel<TW_BF16>;
     return launch(fn, grid, dim3(1024), &p, 0, hip_stream);
 }
@@ -652,6 +759,6 @@ extern "C" int tw_layernorm_grad(const void* dY, int lddy, const void* X, int ld
     const float* pg = p.part_gamma;
     const float* pb = p.part_beta;
     void* args[] = {(void*)&pg, (void*)&pb, (void*)&n_parts, (void*)&n, (void*)&dgamma, (void*)&dbeta};
-    return hipLaunchKernel((const void*)tw_ln_grad_sum_kernel, dim3((unsigned)(((long)N + 63) / 64), 2), dim3(256), args, 0,
+    return hipLaunchKernel((const void*)tw_ln_grad_sum_kernel, dim3((unsigned)(((long)N + 31) / 32), 2), dim3(1024), args, 0,
                            (hipStream_t)hip_stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
 }
