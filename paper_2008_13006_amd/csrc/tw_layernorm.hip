@@ -54,16 +54,19 @@ __device__ __forceinline__ tw_u32x4 pack8(const float (&f)[8]) {
     for (int i = 0; i < 4; ++i) v[i] = (unsigned)tw_cvt<DT>(f[2 * i]) | ((unsigned)tw_cvt<DT>(f[2 * i + 1]) << 16);
     return v;
 }
-// Eight parameters from index c on; those from N on are zero and not read.
-template <int DT, bool TAIL>
-__device__ __forceinline__ void params8(const us* src, int c, int N, float (&f)[8]) {
-    if (!TAIL || c + 8 <= N) {
-        unpack8<DT>(*(const tw_u32x4*)(src + c), f);
-    } else {
+// Eight parameters from index c on as they lie in memory; those from N on are zero and not read, all are `none` without a source.
+template <bool TAIL>
+__device__ __forceinline__ tw_u32x4 params8(const us* src, int c, int N, unsigned none) {
+    if (!src) return tw_u32x4{none, none, none, none};
+    if (c >= N) return tw_u32x4{0u, 0u, 0u, 0u};
+    if (!TAIL || c + 8 <= N) return *(const tw_u32x4*)(src + c);
+    unsigned w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = c + e < N ? tw_to_f32<DT>(src[c + e]) : 0.f;
-    }
+    for (int e = 0; e < 7; ++e)
+        if (c + e < N) w[e >> 1] |= (unsigned)src[c + e] << (16 * (e & 1));
+    return tw_u32x4{w[0], w[1], w[2], w[3]};
 }
+template <int DT> constexpr unsigned ones() { return DT == TW_F16 ? 0x3C003C00u : 0x3F803F80u; }
 template <bool TAIL>
 __device__ __forceinline__ void put8(us* dst, int left, tw_u32x4 v) {   // left: elements up to the row's end
     if (!TAIL || left >= 8) {
@@ -95,6 +98,12 @@ __global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
     __shared__ float red[2][4];
     const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
     const float inv_n = 1.f / (float)p.N;
+    tw_u32x4 ga[PER], be[PER];                               // (asked for with the first row, not behind its statistics)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        ga[i] = params8<TAIL>(p.gamma, 8 * (t + i * TPR), p.N, ones<DT>());
+        be[i] = params8<TAIL>(p.beta, 8 * (t + i * TPR), p.N, 0u);
+    }
     for (long m0 = (long)blockIdx.x * kGroups; m0 < p.M; m0 += (long)gridDim.x * kGroups) {   // (uniform: the barriers are met by all)
         const long m = m0 + grp < p.M ? m0 + grp : p.M - 1;   // (groups behind the last row repeat it and store nothing)
         const bool mine = m0 + grp < p.M;
@@ -141,10 +150,8 @@ __global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
             const int c = 8 * (t + i * TPR);
             if (c < p.N && mine) {
                 float g[8], b[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = 1.f, b[e] = 0.f;
-                if (p.gamma) params8<DT, TAIL>(p.gamma, c, p.N, g);
-                if (p.beta) params8<DT, TAIL>(p.beta, c, p.N, b);
+                unpack8<DT>(ga[i], g);
+                unpack8<DT>(be[i], b);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf(v[i][e] * rstd, g[e], b[e]);
                 put8<TAIL>(out + c, p.N - c, pack8<DT>(v[i]));
@@ -439,11 +446,15 @@ __global__ __launch_bounds__(256) void tw_ln_grad_kernel(const LnGradParams p) {
     for (int i = 0; i < PER; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) sg[i][e] = sb[i][e] = 0.f;
-    for (long m0 = first; m0 < last; m0 += kGroups) {
-        const bool mine = m0 + grp < last;
-        const long m = mine ? m0 + grp : last - 1;
-        const float mean = p.mean[m], rstd = p.rstd[m];
-        tw_u32x4 wx[PER], wd[PER];
+    tw_u32x4 ga[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) ga[i] = params8<TAIL>(p.gamma, 8 * (t + i * TPR), p.N, ones<DT>());
+    tw_u32x4 wx[PER], wd[PER];                               // the row that comes next, on its way while one is worked on
+    float next_mean, next_rstd;
+    auto request = [&](long m0) {
+        const long m = m0 + grp < last ? m0 + grp : last - 1;
+        next_mean = p.mean[m];
+        next_rstd = p.rstd[m];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int c = 8 * (t + i * TPR);
@@ -453,23 +464,27 @@ __global__ __launch_bounds__(256) void tw_ln_grad_kernel(const LnGradParams p) {
                 wd[i] = *(const tw_u32x4*)(p.dy + m * p.lddy + c);
             }
         }
+    };
+    request(first);
+    for (long m0 = first; m0 < last; m0 += kGroups) {
+        const bool mine = m0 + grp < last;
+        const long m = m0 + grp;
+        const float mean = next_mean, rstd = next_rstd;
         float c1 = 0.f, c2 = 0.f;
         float xh[PER][8], g[PER][8];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int c = 8 * (t + i * TPR);
             if (c < p.N) {
-                float f[8], d[8], ga[8];
+                float f[8], d[8], gv[8];
                 unpack8<DT>(wx[i], f);
                 unpack8<DT>(wd[i], d);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ga[e] = 1.f;
-                if (p.gamma) params8<DT, TAIL>(p.gamma, c, p.N, ga);
+                unpack8<DT>(ga[i], gv);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if (TAIL && c + e >= p.N) f[e] = mean, d[e] = 0.f;
                     xh[i][e] = (f[e] - mean) * rstd;
-                    g[i][e] = d[e] * ga[e];
+                    g[i][e] = d[e] * gv[e];
                     if (mine) {
                         sg[i][e] = __builtin_fmaf(d[e], xh[i][e], sg[i][e]);
                         sb[i][e] += d[e];
@@ -479,6 +494,7 @@ __global__ __launch_bounds__(256) void tw_ln_grad_kernel(const LnGradParams p) {
                 }
             }
         }
+        if (m0 + kGroups < last) request(m0 + kGroups);
         if constexpr (TPR == 256) {
             c1 = group_sum<64>(c1);
             c2 = group_sum<64>(c2);
@@ -677,7 +693,7 @@ int launch(const void* fn, dim3 grid, dim3 block, void* params, size_t lds, void
 
 // Workgroups of the backward pass: each leaves N sums of dgamma and of dbeta.
 int grad_parts(int M) {
-    const int want = (M + 15) / 16;
+    const int want = (M + 7) / 8;
     return want < 512 ? want : 512;
 }
 }  // namespace
