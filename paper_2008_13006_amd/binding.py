@@ -474,30 +474,38 @@ def tw_dense_gemm(A, B, C=None, stream=None):
     return C
 
 
+_DT_CODES = {}
+
+
 def _dt_code(t) -> int:
-    torch = _torch()
-    assert t.dtype in (torch.float16, torch.bfloat16)
-    return TW_F16 if t.dtype == torch.float16 else TW_BF16
+    if not _DT_CODES:
+        torch = _torch()
+        _DT_CODES.update({torch.float16: TW_F16, torch.bfloat16: TW_BF16})
+    code = _DT_CODES.get(t.dtype)
+    assert code is not None, "float16 or bfloat16 is wanted"
+    return code
 
 
-def _matrix(t, shape, like) -> int:
+# (Checks of operands, written for few steps: a call of a few microseconds on the GPU takes about as long on the host.)
+def _matrix(t, rows, cols, like) -> int:
     """Checks a matrix operand (GPU, type and device of `like`, unit column stride); its pitch, which one row leaves open."""
-    assert t.is_cuda and t.dtype == like.dtype and t.device == like.device and tuple(t.shape) == tuple(shape)
-    assert shape[1] <= 1 or t.stride(1) == 1
-    return t.stride(0) if shape[0] > 1 and shape[1] > 0 else max(int(shape[1]), 1)
+    assert t.is_cuda and t.dtype == like.dtype and t.get_device() == like.get_device() and t.shape == (rows, cols)
+    ld, unit = t.stride()
+    assert unit == 1 or cols <= 1
+    return ld if rows > 1 and cols > 0 else cols or 1
 
 
-def _matrix8(t, shape, like) -> int:
+def _matrix8(t, rows, cols, like) -> int:
     """The same for entry points whose pitches are multiples of 8: a single row's may be any."""
-    ld = _matrix(t, shape, like)
-    return ld if shape[0] > 1 else -(-ld // 8) * 8
+    ld = _matrix(t, rows, cols, like)
+    return ld if rows > 1 else -(-ld // 8) * 8
 
 
 def _vector(t, n, dtype, like):
     """Checks a vector operand (n elements side by side on the device of `like`); its pointer, None for none."""
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == dtype and t.device == like.device and tuple(t.shape) == (n,) and (n <= 1 or t.stride(0) == 1)
+    assert t.is_cuda and t.dtype == dtype and t.get_device() == like.get_device() and t.shape == (n,) and (n <= 1 or t.stride(0) == 1)
     return t.data_ptr()
 
 
@@ -511,7 +519,7 @@ def tw_gemm_bias_act_add(w: TwWeight, A, R, bias=None, act="none", C=None, strea
     M, N = _row_operands(w, A, C)
     if C is None:
         C = _torch().empty((M, N), dtype=A.dtype, device=A.device)
-    ldr = _matrix(R, (M, N), A)
+    ldr = _matrix(R, M, N, A)
     b = _vector(bias, N, A.dtype, A)
     lda, ldc = A.stride(0), C.stride(0)
     if M <= 1:
@@ -529,7 +537,7 @@ def tw_gemm_t_bias_act_add(w: TwWeight, At, Rt, bias=None, act="none", Ct=None, 
     N = w.info["N"]
     if Ct is None:
         Ct = _torch().empty((N, (M + 63) // 64 * 64), dtype=At.dtype, device=At.device)[:, :M]
-    ldat, ldrt, ldct = _matrix8(At, (K, M), At), _matrix8(Rt, (N, M), At), _matrix8(Ct, (N, M), At)
+    ldat, ldrt, ldct = _matrix8(At, K, M, At), _matrix8(Rt, N, M, At), _matrix8(Ct, N, M, At)
     b = _vector(bias, N, At.dtype, At)
     ws, ws_bytes = w.workspace_for(M)
     _check(_lib.tw_gemm_t_bias_act_add(w._blob_ptr, w.blob_dev.data_ptr(), At.data_ptr(), M, ldat, b, _act_code(act), Rt.data_ptr(), ldrt,
@@ -545,7 +553,7 @@ def tw_dense_gemm_bias_act_add(A, B, R, bias=None, act="none", C=None, stream=No
     N = B.shape[1]
     if C is None:
         C = _new_matrix(M, N, A)
-    lda, ldb, ldr, ldc = _matrix8(A, (M, K), A), _matrix8(B, (K, N), A), _matrix8(R, (M, N), A), _matrix8(C, (M, N), A)
+    lda, ldb, ldr, ldc = _matrix8(A, M, K, A), _matrix8(B, K, N, A), _matrix8(R, M, N, A), _matrix8(C, M, N, A)
     b = _vector(bias, N, A.dtype, A)
     _check(_lib.tw_dense_gemm_bias_act_add(A.data_ptr(), lda, B.data_ptr(), ldb, b, _act_code(act), R.data_ptr(), ldr, C.data_ptr(), ldc,
                                            M, N, K, dt, _stream_ptr(stream)), "tw_dense_gemm_bias_act_add")
@@ -553,14 +561,17 @@ def tw_dense_gemm_bias_act_add(A, B, R, bias=None, act="none", C=None, stream=No
 
 
 def _layernorm(entry, where, X, M, N, gamma, beta, eps, Y, mean, rstd, stream):
-    torch = _torch()
     assert X.is_cuda and X.dim() == 2
     dt = _dt_code(X)
     if Y is None:
         Y = _new_matrix(*X.shape, X)
-    ldx, ldy = _matrix(X, X.shape, X), _matrix(Y, X.shape, X)
+    rows, cols = X.shape
+    ldx, ldy = _matrix(X, rows, cols, X), _matrix(Y, rows, cols, X)
     g, b = _vector(gamma, N, X.dtype, X), _vector(beta, N, X.dtype, X)
-    mu, rs = _vector(mean, M, torch.float32, X), _vector(rstd, M, torch.float32, X)
+    mu = rs = None
+    if mean is not None or rstd is not None:
+        f32 = _torch().float32
+        mu, rs = _vector(mean, M, f32, X), _vector(rstd, M, f32, X)
     _check(entry(X.data_ptr(), ldx, M, N, g, b, float(eps), Y.data_ptr(), ldy, mu, rs, dt, _stream_ptr(stream)), where)
     return Y
 
@@ -589,22 +600,22 @@ def tw_layernorm_grad(dY, X, gamma, mean, rstd, dX=None, dgamma=None, dbeta=None
     assert X.is_cuda and X.dim() == 2
     M, N = X.shape
     dt = _dt_code(X)
-    on = torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
-    with on:                                   # (what is allocated here belongs to the stream that uses it)
-        if dX is None:
-            dX = _new_matrix(M, N, X)
-        if dgamma is None:
-            dgamma = torch.empty(N, dtype=torch.float32, device=X.device)
-        if dbeta is None:
-            dbeta = torch.empty(N, dtype=torch.float32, device=X.device)
-        if workspace is None:
+    if workspace is None:
+        # (allocated on the stream that uses it: its memory goes back to that stream's pool)
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             workspace = torch.empty(tw_layernorm_grad_workspace(M, N), dtype=torch.uint8, device=X.device)
-    assert workspace.is_cuda and workspace.device == X.device and workspace.dtype == torch.uint8 and workspace.is_contiguous()
-    lddy, ldx, lddx = (_matrix(t, (M, N), X) for t in (dY, X, dX))
+    if dX is None:
+        dX = _new_matrix(M, N, X)
+    if dgamma is None:
+        dgamma = torch.empty(N, dtype=torch.float32, device=X.device)
+    if dbeta is None:
+        dbeta = torch.empty(N, dtype=torch.float32, device=X.device)
+    assert workspace.is_cuda and workspace.get_device() == X.get_device() and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+    lddy, ldx, lddx = _matrix(dY, M, N, X), _matrix(X, M, N, X), _matrix(dX, M, N, X)
     g = _vector(gamma, N, X.dtype, X)
-    f32 = [_vector(t, n, torch.float32, X) for t, n in ((mean, M), (rstd, M), (dgamma, N), (dbeta, N))]
-    _check(_lib.tw_layernorm_grad(dY.data_ptr(), lddy, X.data_ptr(), ldx, M, N, g, f32[0], f32[1], dX.data_ptr(), lddx, f32[2], f32[3],
-                                  workspace.data_ptr(), workspace.numel(), dt, _stream_ptr(stream)), "tw_layernorm_grad")
+    f32 = torch.float32
+    _check(_lib.tw_layernorm_grad(dY.data_ptr(), lddy, X.data_ptr(), ldx, M, N, g, _vector(mean, M, f32, X), _vector(rstd, M, f32, X), dX.data_ptr(),
+                                  lddx, _vector(dgamma, N, f32, X), _vector(dbeta, N, f32, X), workspace.data_ptr(), workspace.numel(), dt, _stream_ptr(stream)), "tw_layernorm_grad")
     return dX, dgamma, dbeta
 
 
@@ -620,8 +631,8 @@ def tw_attention(Q, K, V, seq_start, heads: int, kv_heads: Optional[int] = None,
     dt = _dt_code(Q)
     if O is None:
         O = _new_matrix(M, heads * d, Q)
-    ldq, ldo = _matrix(Q, (M, heads * d), Q), _matrix(O, (M, heads * d), Q)
-    ldk, ldv = _matrix(K, (M, kv_heads * d), Q), _matrix(V, (M, kv_heads * d), Q)
+    ldq, ldo = _matrix8(Q, M, heads * d, Q), _matrix8(O, M, heads * d, Q)
+    ldk, ldv = _matrix8(K, M, kv_heads * d, Q), _matrix8(V, M, kv_heads * d, Q)
     n_seqs, starts = 0, None
     if seq_start is not None:
         assert seq_start.dim() == 1 and seq_start.numel() >= 1
