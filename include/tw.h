@@ -261,7 +261,7 @@ int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, const void* 
  *   bias, act  as in tw_gemm_bias_act (NULL and TW_ACT_NONE: the plain product plus R)
  * The sum of the fp32 result and R is rounded once to the storage type.  A pruned column n of C holds act(bias[n]) + R[m, n].
  * Everything else as tw_gemm_bias_act; TW_ERR_ARG also for a null R, ldr < N, R = C with another pitch; TW_ERR_UNSUPPORTED also for
- * ldr >= 2^23 and for R = C where a TEW blob rules it out. */
+ * R = C where a TEW blob rules it out. */
 int tw_gemm_bias_act_add(const void* blob_host, const void* blob_dev, const void* A, int M, int lda,
                          const void* bias, tw_act act, const void* R, int ldr, void* C, int ldc, void* workspace,
                          size_t ws_bytes, void* hip_stream);
