@@ -352,12 +352,12 @@ int tw_layernorm_grad(const void* dY, int lddy, const void* X, int ldx, int M, i
  *   head_dim   a multiple of 8, at most 128
  *   scale      >= 0 and finite (1 / sqrt(head_dim) as a rule)
  * Scores, softmax statistics and sums are fp32; the weights p are rounded to dt for the product with V, O is rounded once.  A token that a row
- * does not see leaves it untouched, whatever its values; non-finite scores or values that it sees give what the formula gives
- * (NaN, or inf where the infinities agree).
+ * does not see leaves it untouched, whatever its values; non-finite scores or values that it sees give what the formula gives in
+ * fp32 (a weight that underflows to zero beside an infinite value: NaN or that infinity).
  * M >= 0 (M = 0 enqueues nothing).  One kernel, no workspace; it can be recorded into a HIP graph (the lengths are read when it runs).
  * Errors: TW_ERR_ARG (null pointer, negative M or n_seqs, heads not a multiple of kv_heads, pitch too small, scale, unknown dt, no
  * seq_start and n_seqs > 1), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED (head_dim; ldk or ldv of 2^24 and more; heads * ceil(M / 128) of 2^24
- * and more), TW_ERR_HIP. */
+ * and more; a scale above 2.3e38), TW_ERR_HIP. */
 int tw_attention(const void* Q, int ldq, const void* K, int ldk, const void* V, int ldv, void* O, int ldo, int M,
                  const int* seq_start, int n_seqs, int heads, int kv_heads, int head_dim, float scale, int causal, tw_dtype dt,
                  void* hip_stream);

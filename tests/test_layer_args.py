@@ -56,6 +56,11 @@ def test_layernorm_grad_refusals():
     assert tw.tw_layernorm_grad_workspace(1, 5) == 4 * (2 * 5 + 2) and tw.tw_layernorm_grad_workspace(10 ** 6, 768) == 4 * (1024 * 768 + 2 * 10 ** 6)
 
 
+def test_layernorm_grad_workspace_of_very_many_rows():
+    rows = 2 ** 31 - 1
+    assert tw.tw_layernorm_grad_workspace(rows, 8) == 4 * (512 * 2 * 8 + 2 * rows)
+
+
 def attention(Q=P, ldq=128, K=P, ldk=64, V=P, ldv=64, O=P, ldo=128, M=4, seq_start=P, n_seqs=1, heads=2, kv_heads=1, d=64, scale=0.125, causal=1, dt=0):
     return tw._lib.tw_attention(Q, ldq, K, ldk, V, ldv, O, ldo, M, seq_start, n_seqs, heads, kv_heads, d, scale, causal, dt, None)
 
@@ -72,6 +77,12 @@ def test_attention_refusals():
         assert attention(**kw) == want, kw
     assert attention(M=0, Q=None, K=None, V=None, O=None) == 0
     assert attention(n_seqs=0) == 0                              # no sequence, no row
+
+
+def test_attention_scale_out_of_range():
+    # the kernel multiplies by scale * log2 e, which has to be finite as well
+    assert attention(scale=3e38) == UNSUPPORTED
+    assert attention(scale=2.3e38, M=0) == 0
 
 
 def test_add_refusals():
