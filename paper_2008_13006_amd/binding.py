@@ -491,7 +491,7 @@ def _matrix(t, rows, cols, like) -> int:
     """Checks a matrix operand (GPU, type and device of `like`, unit column stride); its pitch, which one row leaves open."""
     assert t.is_cuda and t.dtype == like.dtype and t.get_device() == like.get_device() and t.shape == (rows, cols)
     ld, unit = t.stride()
-    assert unit == 1 or cols <= 1
+    assert (unit == 1 or cols <= 1) and ld <= 0x7FFFFFFF and rows <= 0x7FFFFFFF      # (ctypes would cut them to 32 bits)
     return ld if rows > 1 and cols > 0 else cols or 1
 
 

@@ -113,3 +113,22 @@ def test_add_refusals():
                      (dict(dt=2), ARG), (dict(act=9), ARG), (dict(K=0), ARG), (dict(M=-1), ARG)]:
         assert dense(**kw) == want, kw
     assert row(M=0) == 0 and col(M=0) == 0 and dense(M=0) == 0
+
+
+def test_sizes_beyond_32_bits_are_not_cut():
+    class Operand:                                               # what the binding looks at
+        is_cuda, dtype = True, torch.float16
+
+        def __init__(self, rows, cols, ld):
+            self.shape, self.ld = (rows, cols), ld
+
+        def get_device(self):
+            return 0
+
+        def stride(self):
+            return self.ld, 1
+
+    for rows, cols, ld in [(2 ** 32 + 4, 8, 8), (4, 8, 2 ** 32 + 8), (4, 2 ** 31 + 8, 2 ** 31 + 8)]:
+        with pytest.raises(AssertionError):
+            tw._matrix(Operand(rows, cols, ld), rows, cols, Operand(rows, cols, ld))
+    assert tw._matrix(Operand(4, 8, 2 ** 31 - 8), 4, 8, Operand(4, 8, 8)) == 2 ** 31 - 8
