@@ -259,3 +259,21 @@ def test_streams_and_graphs():
         got = o.clone()
         assert torch.equal(got, tw.tw_attention(q, k, v, seq, heads, 2))
         check(got, q, k, v, [0, cut, 500], heads, 2, 0.125, True)
+
+
+@pytest.mark.parametrize("heads,d,lens,before,after", [(16, 80, [4100, 37, 0, 2500, 900, 1], 0, 0), (16, 72, [500] * 12, 150, 333), (5, 104, [9000, 1, 5500], 3, 0),
+                                                       (8, 128, [1, 8500, 0], 0, 700), (3, 72, [20000, 12768], 0, 0)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_tiles_of_different_lengths(heads, d, lens, before, after, causal):
+    """More workgroups than run at once, prompts of several tiles: tiles start in the order of their numbers of keys.  Every row that belongs to a
+    sequence is written, the others are left; in place gives the same bits."""
+    starts = starts_of(lens, before)
+    M = starts[-1] + after
+    q, k, v = make(M, heads, 1, d, "bf16", 21)
+    o = torch.full((M, heads * d), 7.0, dtype=torch.bfloat16, device="cuda")
+    run(q, k, v, starts, heads, 1, causal, O=o)
+    assert bool((o[:before] == 7.0).all()) and bool((o[starts[-1]:] == 7.0).all())
+    check(o, q, k, v, starts, heads, 1, d ** -0.5, causal)
+    again = q.clone()
+    run(again, k, v, starts, heads, 1, causal, O=again)
+    assert torch.equal(again[before:starts[-1]], o[before:starts[-1]]) and torch.equal(again[:before], q[:before])
