@@ -2535,9 +2535,10 @@ __global__ __launch_bounds__(kThreads) void tw_part_kernel(const TwGemmParams p)
 }  // namespace
 
 // ---- kernel tables
-// The kernels can be compiled as twelve translation units (-DTW_PART=1..4: fp16 / bf16 x plain / fused epilogue, 5..8:
-// the same for TEW blobs, 9..12: fp16, bf16 with the adding epilogue, then the same for TEW blobs) beside the host code (-DTW_PART=0), so that a build runs them in parallel; without TW_PART one unit holds
-// everything.  The tables hand out host-side kernel addresses, so no type of this file crosses a unit boundary.
+// The kernels can be compiled as twelve translation units (-DTW_PART=1..4: fp16 / bf16 x plain / fused epilogue, 5..8: the same for
+// TEW blobs, 9..12: fp16, bf16 with the adding epilogue, then the same for TEW blobs) beside the host code (-DTW_PART=0), so that a
+// build runs them in parallel; without TW_PART one unit holds everything.  The tables hand out host-side kernel addresses, so no type of
+// this file crosses a unit boundary.
 namespace tw_parts {
 // (nta: the streamed kernels' variant whose requests for activations carry the streaming hint)
 // (EW: the variant with the code of the element-wise residual, for TEW blobs)
