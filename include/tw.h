@@ -306,7 +306,9 @@ int tw_dense_gemm_bias_act_add(const void* A, int lda, const void* B, int ldb, c
  *   gamma, beta  device, N elements of type dt each, or NULL for ones / zeros
  *   eps          >= 0 and finite
  *   mean, rstd   device, M floats each for a backward pass, or NULL
- * Sums are fp32, the variance is taken about the mean, Y is rounded once.  Non-finite values stay within their row.
+ * Sums are fp32, Y is rounded once.  The mean is taken in two steps, the second about the first, so that rows which hardly vary keep what
+ * they vary by whatever the size of their values (a constant row gives beta); `mean` receives it rounded to fp32.  Non-finite values stay
+ * within their row.
  * M >= 0 (M = 0 enqueues nothing).  One kernel, no workspace; it can be recorded into a HIP graph.
  * Errors: TW_ERR_ARG (null X or Y, negative M, N <= 0, pitch too small, unknown dt, eps), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED
  * (N above 2^24 - 256; tw_layernorm_t also M above 2^27 - 64), TW_ERR_HIP. */

@@ -6,7 +6,13 @@
 //     dx = rstd (g - mean_n g - xh mean_n(g xh)),   dgamma[n] = sum_m dy xh,   dbeta[n] = sum_m dy
 //
 // All of it is bound by memory: forward 4 bytes an element, backward 6.  A row is read once and waits in registers for its
-// statistics (the variance is taken about the mean, not as a difference of two large sums); everything is fp32, rounded once at the store.
+// statistics; everything is fp32, rounded once at the store.
+//
+// The mean comes in two steps, mu0 = fl(sum x / N) and the rest r = sum (x - mu0) / N: a step of fp32 at 60000 is 0.004, which the 1 / sqrt(eps) of a
+// row that hardly varies makes 1.2.  x - mu0 is exact for such rows, so (x - mu0) - r has the error of its own size, not of x's, and the variance
+// is sum (x - mu0)^2 / N - r^2, the difference of a sum about the mean and next to nothing (for most rows r is below a step of mu0).
+// The first step is a division: a constant row whose sum is exact has itself as its mean then, and the product with fl(1 / N)
+// misses it for many N.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -31,11 +37,33 @@ struct LnParams {
     int stream;                 // rows of y start on 128-byte boundaries: whole lines go out as streaming stores
 };
 
+// Lanes exchanged by the vector unit alone: within rows of 16 lanes (CTRL: 0xB1 lane ^ 1, 0x4E lane ^ 2, 0x141 the other four of eight, 0x140 the other
+// eight, 0x128 lane ^ 8), and whole rows or halves.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+// In lanes of even rows (of the lower half) a summed over the pair of rows (both halves), in the others b.
+__device__ __forceinline__ float rows_sum(float a, float b) {
+    const auto both = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned even = both[0], odd = both[1];            // (copies: the builtin cast of a vector's element takes the first one)
+    return __builtin_bit_cast(float, even) + __builtin_bit_cast(float, odd);
+}
+__device__ __forceinline__ float halves_sum(float a, float b) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned low = both[0], high = both[1];
+    return __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
+}
 // Sum over groups of TPR consecutive lanes, the same bits in every lane of the group.
 template <int TPR>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-    for (int s = 1; s < TPR && s < 64; s <<= 1) v += __shfl_xor(v, s);
+    static_assert(TPR >= 16, "");
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    v += dpp<0x140>(v);
+    if constexpr (TPR >= 32) v = rows_sum(v, v);
+    if constexpr (TPR >= 64) v = halves_sum(v, v);
     return v;
 }
 
@@ -78,9 +106,9 @@ __device__ __forceinline__ void put8(us* dst, int left, tw_u32x4 v) {   // left:
     }
 }
 
-// Sum over the TPR threads of a row: lanes of a wave, or the four waves of a workgroup (`red`: two rows of four floats, used in turn).
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float (&red)[2][4], int turn) {
+// Sum over the TPR threads of a row: lanes of a wave, or the four waves of a workgroup (`red`: rows of four floats, used in turn).
+template <int TPR, int ROWS>
+__device__ __forceinline__ float row_sum(float v, float (&red)[ROWS][4], int turn) {
     v = group_sum<TPR>(v);
     if constexpr (TPR == 256) {
         if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = v;
@@ -90,13 +118,34 @@ __device__ __forceinline__ float row_sum(float v, float (&red)[2][4], int turn) 
     return v;
 }
 
+// The same for two sums at once: rows `turn` and `turn` + 1 of `red`.
+template <int TPR>
+__device__ __forceinline__ void row_sum2(float& v, float& w, float (&red)[3][4], int turn) {
+    v = group_sum<TPR>(v);
+    w = group_sum<TPR>(w);
+    if constexpr (TPR == 256) {
+        if ((threadIdx.x & 63) == 0) {
+            red[turn][threadIdx.x >> 6] = v;
+            red[turn + 1][threadIdx.x >> 6] = w;
+        }
+        __syncthreads();
+        v = (red[turn][0] + red[turn][1]) + (red[turn][2] + red[turn][3]);
+        w = (red[turn + 1][0] + red[turn + 1][1]) + (red[turn + 1][2] + red[turn + 1][3]);
+    }
+}
+// 1 / deviation from the sums of squares about a value that misses the mean by `rest`.  (The comparison keeps NaN.)
+__device__ __forceinline__ float deviation(float squares, float rest, float inv_n, float eps) {
+    const float var = squares * inv_n - rest * rest;
+    return 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);
+}
+
 // Row-major, 16-byte pieces.  TPR threads of a workgroup of 256 share a row, thread t of them the pieces t, t + TPR, .. (PER of
 // them); TAIL: N is no multiple of 8, the last piece reaches into the row's pitch.
 // (16384 x 4096: 40 us, 6.7 TB/s with part of the data in the last-level cache; 512 x 768: 3.6 us, an empty kernel takes 2.4.)
 template <int DT, int TPR, int PER, bool TAIL>
 __global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
     constexpr int kGroups = 256 / TPR;
-    __shared__ float red[2][4];
+    __shared__ float red[3][4];
     const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
     const float inv_n = 1.f / (float)p.N;
     tw_u32x4 ga[PER], be[PER];                               // (asked for with the first row, not behind its statistics)
@@ -127,8 +176,8 @@ __global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
                 s += v[i][e];
             }
         }
-        const float mean = row_sum<TPR>(s, red, 0) * inv_n;
-        float q = 0.f;
+        const float mean = row_sum<TPR>(s, red, 0) / (float)p.N;
+        float q = 0.f, r = 0.f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int c = 8 * (t + i * TPR);
@@ -136,13 +185,18 @@ __global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     v[i][e] -= mean;
-                    if (!TAIL || c + e < p.N) q = __builtin_fmaf(v[i][e], v[i][e], q);
+                    if (!TAIL || c + e < p.N) {
+                        q = __builtin_fmaf(v[i][e], v[i][e], q);
+                        r += v[i][e];
+                    }
                 }
             }
         }
-        const float rstd = 1.f / sqrtf(row_sum<TPR>(q, red, 1) * inv_n + p.eps);
+        row_sum2<TPR>(q, r, red, 1);
+        r *= inv_n;
+        const float rstd = deviation(q, r, inv_n, p.eps);
         if (mine && t == 0) {
-            if (p.mean) p.mean[m] = mean;
+            if (p.mean) p.mean[m] = mean + r;
             if (p.rstd) p.rstd[m] = rstd;
         }
         us* out = p.y + m * p.ldy;
@@ -154,7 +208,7 @@ __global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
                 unpack8<DT>(ga[i], g);
                 unpack8<DT>(be[i], b);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf(v[i][e] * rstd, g[e], b[e]);
+                for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf((v[i][e] - r) * rstd, g[e], b[e]);
                 put8<TAIL>(out + c, p.N - c, pack8<DT>(v[i]));
             }
         }
@@ -165,27 +219,30 @@ __global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
 // first).
 template <int DT>
 __global__ __launch_bounds__(256) void tw_ln_any_kernel(const LnParams p) {
-    __shared__ float red[2][4];
+    __shared__ float red[3][4];
     const float inv_n = 1.f / (float)p.N;
     for (long m = blockIdx.x; m < p.M; m += gridDim.x) {
         const us* row = p.x + m * p.ldx;
         float s = 0.f;
         for (int c = threadIdx.x; c < p.N; c += 256) s += tw_to_f32<DT>(row[c]);
-        const float mean = row_sum<256>(s, red, 0) * inv_n;
-        float q = 0.f;
+        const float mean = row_sum<256>(s, red, 0) / (float)p.N;
+        float q = 0.f, r = 0.f;
         for (int c = threadIdx.x; c < p.N; c += 256) {
             const float d = tw_to_f32<DT>(row[c]) - mean;
             q = __builtin_fmaf(d, d, q);
+            r += d;
         }
-        const float rstd = 1.f / sqrtf(row_sum<256>(q, red, 1) * inv_n + p.eps);
+        row_sum2<256>(q, r, red, 1);
+        r *= inv_n;
+        const float rstd = deviation(q, r, inv_n, p.eps);
         if (threadIdx.x == 0) {
-            if (p.mean) p.mean[m] = mean;
+            if (p.mean) p.mean[m] = mean + r;
             if (p.rstd) p.rstd[m] = rstd;
         }
         us* out = p.y + m * p.ldy;
         for (int c = threadIdx.x; c < p.N; c += 256) {
             const float g = p.gamma ? tw_to_f32<DT>(p.gamma[c]) : 1.f, b = p.beta ? tw_to_f32<DT>(p.beta[c]) : 0.f;
-            out[c] = tw_cvt<DT>(__builtin_fmaf((tw_to_f32<DT>(row[c]) - mean) * rstd, g, b));
+            out[c] = tw_cvt<DT>(__builtin_fmaf(((tw_to_f32<DT>(row[c]) - mean) - r) * rstd, g, b));
         }
     }
 }
@@ -198,15 +255,43 @@ __device__ __forceinline__ void forget(tw_u32x4 (&w)[PER]) {
     for (int i = 0; i < PER; ++i) asm volatile("" : "+v"(w[i]));
 }
 
-constexpr int PCS = 8;                                       // 16-byte pieces of a row that a workgroup takes
+constexpr int PCS = 8;                                       // 16-byte pieces of a row that a workgroup takes: a token for each lane of a wave
+// Statistics of the block's tokens.  A lane has sums of eight tokens over its rows; `leave` sums them over the eight lanes of the wave that hold the
+// same piece, each of which ends with one token and leaves it in LDS, where the block's tokens lie in order.  Behind a barrier lane t of every wave has
+// `waves_sum` of token t, and what all lanes make of those goes round through the wave's own part of LDS: `give` puts a lane's value there,
+// `get` takes the eight of its piece.  (Sums of all eight
+// tokens in every lane, 24 exchanges through LDS and 64 reads of it each: 17.2 us on 16384 x 768, 13.4 so.)
+__device__ __forceinline__ void leave(const float (&s)[8], float (&red)[8 * PCS], int lane) {
+    const float a = halves_sum(s[0], s[4]), b = halves_sum(s[1], s[5]), c = halves_sum(s[2], s[6]), d = halves_sum(s[3], s[7]);
+    float x = rows_sum(a, c), y = rows_sum(b, d);
+    x += dpp<0x128>(x);                                      // (both by every lane: lanes that a branch leaves out give nothing)
+    y += dpp<0x128>(y);
+    red[8 * (lane % PCS) + 4 * (lane >> 5) + 2 * ((lane >> 4) & 1) + ((lane >> 3) & 1)] = (lane & 8) == 0 ? x : y;
+}
+template <int WAVES>
+__device__ __forceinline__ float waves_sum(const float (&red)[WAVES][8 * PCS], int lane) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) s += red[k][lane];
+    return s;
+}
+__device__ __forceinline__ void give(float v, float (&own)[8 * PCS], int lane) { own[lane] = v; }
+__device__ __forceinline__ void get(float (&v)[8], const float (&own)[8 * PCS], int lane) {
+    asm volatile("" ::: "memory");                           // (the LDS executes a wave's instructions in order)
+    const float4 a = *(const float4*)&own[8 * (lane % PCS)], b = *(const float4*)&own[8 * (lane % PCS) + 4];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    asm volatile("" ::: "memory");
+}
 // Transposed boundary: features are rows, tokens columns.  A workgroup takes 8 * PCS tokens, a lane the 16-byte piece lane % PCS of the rows
 // lane / PCS + 64 / PCS * wave + 64 / PCS * WAVES * i, PER of them, which wait in registers as they were read.  A token's sums meet across
 // the lanes of a wave that hold its piece and, through LDS, across the waves.  64 tokens are whole 128-byte lines, which go out as
-// streaming stores: 16384 x 768 in 13.7 us (3.7 TB/s); 32 tokens a workgroup, twice as many of them: 24.7 us, half lines.
+// streaming stores: 16384 x 768 in 13.4 us (3.8 TB/s); 32 tokens a workgroup, twice as many of them: 24.7 us, half lines.
 template <int DT, int WAVES, int PER>
 __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
     constexpr int kRows = 64 / PCS * WAVES;
-    __shared__ float red[2][WAVES][8 * PCS];
+    __shared__ float red[3][WAVES][8 * PCS];
+    __shared__ __attribute__((aligned(16))) float own[WAVES][2][8 * PCS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pc = lane % PCS;
     const long m0 = (long)blockIdx.x * (8 * PCS) + 8 * pc;
     const int n0 = 64 / PCS * wave + lane / PCS;
@@ -218,25 +303,7 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
         w[i] = tw_u32x4{0u, 0u, 0u, 0u};
         if (here && n0 + kRows * i < p.N) w[i] = tw_load16_stream(p.x + (long)(n0 + kRows * i) * p.ldx + m0);
     }
-    auto across = [&](float (&s)[8], int turn) {             // sums of the eight tokens over all rows
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-#pragma unroll
-            for (int k = PCS; k < 64; k <<= 1) s[e] += __shfl_xor(s[e], k);
-        }
-        if (lane < PCS) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) red[turn][wave][8 * pc + e] = s[e];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s[e] = 0.f;
-#pragma unroll
-            for (int k = 0; k < WAVES; ++k) s[e] += red[turn][k][8 * pc + e];
-        }
-    };
-    float mean[8] = {}, rstd[8] = {};
+    float mean[8] = {}, rstd[8] = {}, rest[8] = {};
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         float f[8];
@@ -245,10 +312,12 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
         for (int e = 0; e < 8; ++e) mean[e] += f[e];
         __builtin_amdgcn_sched_barrier(0);
     }
-    across(mean, 0);
+    leave(mean, red[0][wave], lane);
+    __syncthreads();
+    const float my_mean = waves_sum(red[0], lane) / (float)p.N;
+    give(my_mean, own[wave][0], lane);
+    get(mean, own[wave][0], lane);
     forget(w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mean[e] *= inv_n;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         float f[8];
@@ -258,23 +327,26 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
             for (int e = 0; e < 8; ++e) {
                 const float d = f[e] - mean[e];
                 rstd[e] = __builtin_fmaf(d, d, rstd[e]);
+                rest[e] += d;
             }
         }
         __builtin_amdgcn_sched_barrier(0);
     }
-    across(rstd, 1);
-    forget(w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) rstd[e] = 1.f / sqrtf(rstd[e] * inv_n + p.eps);
-    if (!here) return;
-    if (threadIdx.x < PCS) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (m0 + e < p.M) {
-                if (p.mean) p.mean[m0 + e] = mean[e];
-                if (p.rstd) p.rstd[m0 + e] = rstd[e];
-            }
+    leave(rstd, red[1][wave], lane);
+    leave(rest, red[2][wave], lane);
+    __syncthreads();
+    const float my_rest = waves_sum(red[2], lane) * inv_n, my_rstd = deviation(waves_sum(red[1], lane), my_rest, inv_n, p.eps);
+    const long token = (long)blockIdx.x * (8 * PCS) + lane;
+    if (wave == 0 && token < p.M) {
+        if (p.mean) p.mean[token] = my_mean + my_rest;
+        if (p.rstd) p.rstd[token] = my_rstd;
     }
+    give(my_rstd, own[wave][0], lane);
+    give(my_rest, own[wave][1], lane);
+    get(rstd, own[wave][0], lane);
+    get(rest, own[wave][1], lane);
+    forget(w);
+    if (!here) return;
     const int left = p.M - m0 < 8 ? (int)(p.M - m0) : 8;
 #pragma unroll
     for (int i0 = 0; i0 < PER; i0 += 4) {                    // (four rows at a time: unpacked all at once they would not fit)
@@ -291,7 +363,7 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
             float f[8];
             unpack8<DT>(w[i0 + i], f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf((f[e] - mean[e]) * rstd[e], g[i], b[i]);
+            for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(((f[e] - mean[e]) - rest[e]) * rstd[e], g[i], b[i]);
             if (n >= p.N) continue;
             if (p.stream && left == 8) tw_store16_stream(p.y + (long)n * p.ldy + m0, pack8<DT>(f));
             else put8<true>(tw_opaque(p.y) + (long)n * p.ldy + m0, left, pack8<DT>(f));
@@ -304,30 +376,13 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
 template <int DT>
 __global__ __launch_bounds__(1024) void tw_ln_t_loop_kernel(const LnParams p) {
     constexpr int WAVES = 16, kRows = 64 / PCS * WAVES;
-    __shared__ float red[2][WAVES][8 * PCS];
+    __shared__ float red[3][WAVES][8 * PCS];
+    __shared__ __attribute__((aligned(16))) float own[WAVES][2][8 * PCS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pc = lane % PCS;
     const long m0 = (long)blockIdx.x * (8 * PCS) + 8 * pc;
     const int n0 = 64 / PCS * wave + lane / PCS;
     const bool here = m0 < p.M;
     const float inv_n = 1.f / (float)p.N;
-    auto across = [&](float (&s)[8], int turn) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-#pragma unroll
-            for (int k = PCS; k < 64; k <<= 1) s[e] += __shfl_xor(s[e], k);
-        }
-        if (lane < PCS) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) red[turn][wave][8 * pc + e] = s[e];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s[e] = 0.f;
-#pragma unroll
-            for (int k = 0; k < WAVES; ++k) s[e] += red[turn][k][8 * pc + e];
-        }
-    };
     auto rows = [&](auto use) {                              // use(row, its piece) for this lane's rows
         for (int n = n0; n < p.N; n += 4 * kRows) {
             tw_u32x4 w[4];
@@ -341,41 +396,49 @@ __global__ __launch_bounds__(1024) void tw_ln_t_loop_kernel(const LnParams p) {
                 if (n + i * kRows < p.N) use(n + i * kRows, w[i]);
         }
     };
-    float mean[8] = {}, rstd[8] = {};
+    float mean[8] = {}, rstd[8] = {}, rest[8] = {};
     rows([&](int, tw_u32x4 w) {
         float f[8];
         unpack8<DT>(w, f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) mean[e] += f[e];
     });
-    across(mean, 0);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mean[e] *= inv_n;
+    leave(mean, red[0][wave], lane);
+    __syncthreads();
+    const float my_mean = waves_sum(red[0], lane) / (float)p.N;
+    give(my_mean, own[wave][0], lane);
+    get(mean, own[wave][0], lane);
     rows([&](int, tw_u32x4 w) {
         float f[8];
         unpack8<DT>(w, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rstd[e] = __builtin_fmaf(f[e] - mean[e], f[e] - mean[e], rstd[e]);
+        for (int e = 0; e < 8; ++e) {
+            const float d = f[e] - mean[e];
+            rstd[e] = __builtin_fmaf(d, d, rstd[e]);
+            rest[e] += d;
+        }
     });
-    across(rstd, 1);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) rstd[e] = 1.f / sqrtf(rstd[e] * inv_n + p.eps);
-    if (!here) return;
-    if (threadIdx.x < PCS) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (m0 + e < p.M) {
-                if (p.mean) p.mean[m0 + e] = mean[e];
-                if (p.rstd) p.rstd[m0 + e] = rstd[e];
-            }
+    leave(rstd, red[1][wave], lane);
+    leave(rest, red[2][wave], lane);
+    __syncthreads();
+    const float my_rest = waves_sum(red[2], lane) * inv_n, my_rstd = deviation(waves_sum(red[1], lane), my_rest, inv_n, p.eps);
+    const long token = (long)blockIdx.x * (8 * PCS) + lane;
+    if (wave == 0 && token < p.M) {
+        if (p.mean) p.mean[token] = my_mean + my_rest;
+        if (p.rstd) p.rstd[token] = my_rstd;
     }
+    give(my_rstd, own[wave][0], lane);
+    give(my_rest, own[wave][1], lane);
+    get(rstd, own[wave][0], lane);
+    get(rest, own[wave][1], lane);
+    if (!here) return;
     const int left = p.M - m0 < 8 ? (int)(p.M - m0) : 8;
     rows([&](int n, tw_u32x4 w) {
         const float g = p.gamma ? tw_to_f32<DT>(p.gamma[n]) : 1.f, b = p.beta ? tw_to_f32<DT>(p.beta[n]) : 0.f;
         float f[8];
         unpack8<DT>(w, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf((f[e] - mean[e]) * rstd[e], g, b);
+        for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(((f[e] - mean[e]) - rest[e]) * rstd[e], g, b);
         put8<true>(p.y + (long)n * p.ldy + m0, left, pack8<DT>(f));
     });
 }
@@ -383,36 +446,42 @@ __global__ __launch_bounds__(1024) void tw_ln_t_loop_kernel(const LnParams p) {
 // Transposed boundary, any pitch, alignment and N: a lane per token, the rows dealt out to the waves, read three times.
 template <int DT>
 __global__ __launch_bounds__(1024) void tw_ln_t_any_kernel(const LnParams p) {
-    __shared__ float red[2][16][64];
+    __shared__ float red[3][16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long m = (long)blockIdx.x * 64 + lane;
     const long mc = m < p.M ? m : p.M - 1;
     const float inv_n = 1.f / (float)p.N;
-    auto across = [&](float s, int turn) {
-        red[turn][wave][lane] = s;
-        __syncthreads();
-        s = 0.f;
+    auto sum = [&](int turn) {
+        float s = 0.f;
 #pragma unroll
         for (int k = 0; k < 16; ++k) s += red[turn][k][lane];
         return s;
     };
     float s = 0.f;
     for (int n = wave; n < p.N; n += 16) s += tw_to_f32<DT>(p.x[(long)n * p.ldx + mc]);
-    const float mean = across(s, 0) * inv_n;
+    red[0][wave][lane] = s;
+    __syncthreads();
+    const float mean = sum(0) / (float)p.N;
+    float rest = 0.f;
     s = 0.f;
     for (int n = wave; n < p.N; n += 16) {
         const float d = tw_to_f32<DT>(p.x[(long)n * p.ldx + mc]) - mean;
         s = __builtin_fmaf(d, d, s);
+        rest += d;
     }
-    const float rstd = 1.f / sqrtf(across(s, 1) * inv_n + p.eps);
+    red[1][wave][lane] = s;
+    red[2][wave][lane] = rest;
+    __syncthreads();
+    rest = sum(2) * inv_n;
+    const float rstd = deviation(sum(1), rest, inv_n, p.eps);
     if (m >= p.M) return;
     if (wave == 0) {
-        if (p.mean) p.mean[m] = mean;
+        if (p.mean) p.mean[m] = mean + rest;
         if (p.rstd) p.rstd[m] = rstd;
     }
     for (int n = wave; n < p.N; n += 16) {
         const float g = p.gamma ? tw_to_f32<DT>(p.gamma[n]) : 1.f, b = p.beta ? tw_to_f32<DT>(p.beta[n]) : 0.f;
-        p.y[(long)n * p.ldy + m] = tw_cvt<DT>(__builtin_fmaf((tw_to_f32<DT>(p.x[(long)n * p.ldx + m]) - mean) * rstd, g, b));
+        p.y[(long)n * p.ldy + m] = tw_cvt<DT>(__builtin_fmaf(((tw_to_f32<DT>(p.x[(long)n * p.ldx + m]) - mean) - rest) * rstd, g, b));
     }
 }
 

@@ -286,3 +286,66 @@ def test_streams_and_graphs():
         both()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((y, dx, dgamma, dbeta), got))
+
+
+def both_boundaries(x, gamma, beta, aligned=True):
+    """(y, mean, rstd, c) row-major and from the transposed boundary, by the kernels for aligned operands or by those for any.  c: the length
+    of the chain of additions in a sum, and a few operations beside it.  Columns of any alignment: a thread adds every 16th value, then 16
+    threads' sums are added; aligned ones beyond 2048: every 128th, three levels of a tree, 16 sums."""
+    M, N = x.shape
+    for transposed in (False, True):
+        src = x.t() if transposed else x
+        a, _ = make(*src.shape, x.dtype, 8, 0 if aligned else 1)
+        a.copy_(src)
+        y, _ = make(*src.shape, x.dtype)
+        mean, rstd = (torch.empty(M, device="cuda") for _ in range(2))
+        (tw.tw_layernorm_t if transposed else tw.tw_layernorm)(a, gamma, beta, 1e-5, y, mean, rstd)
+        c = max(depth(N), (-(-N // 128) + 3 if aligned else -(-N // 16)) + 16) if transposed else depth(N)
+        yield y.t() if transposed else y, mean, rstd, c + 8
+
+
+@pytest.mark.parametrize("aligned", [True, False])
+@pytest.mark.parametrize("N", [7, 100, 1000, 1792, 2047, 3584, 5001, 20001])
+def test_constant_rows(N, aligned):
+    """Every element is its row's mean: what is left is the offset, whatever the value, its size and the number of features.  (A step of fp32 at
+    60000 is 0.004, and 1 / sqrt(eps) makes 1.2 of it.)"""
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    for t, values in ((torch.float16, (60000.0, -65504.0, 2049.0 * 16, 0.1, 1027.0)), (torch.bfloat16, (60000.0, -1e20, 129.0 * 512, 3.3))):
+        x = torch.tensor(values, device="cuda").to(t)[:, None].expand(-1, N).contiguous()
+        gamma = (1 + 0.2 * torch.randn(N, generator=gen, device="cuda")).to(t)
+        beta = (0.5 + torch.rand(N, generator=gen, device="cuda")).to(t)
+        for y, mean, rstd, c in both_boundaries(x, gamma, beta, aligned):
+            assert torch.equal(y, beta.expand_as(y))
+            assert torch.equal(mean, x[:, 0].float())
+            # 1 / sqrt(eps) with eps in 32 bits: the root and the quotient are off by half a step each.  Up to 8192 features the sums of a constant
+            # are exact (13 + 11 bits); beyond, the first mean may be off by c U |x|, and c U of that squared is left of the variance
+            off = 0 if N <= 8192 else c * U * x[:, 0].double().abs()
+            assert bool(((rstd.double() * 1e-5 ** 0.5 - 1).abs() <= 4 * U + 0.5 * c * U * off ** 2 / 1e-5).all())
+
+
+@pytest.mark.parametrize("aligned", [True, False])
+@pytest.mark.parametrize("N", [100, 1000, 1792, 3001, 20001])
+def test_rows_that_hardly_vary(N, aligned):
+    """A few elements one step beside a large common value: the mean's rounding to fp32 must not show in what is normalised.
+
+    The first mean is off by c U mean|x| at most, c the length of the chain of sums.  x less that is exact (the two lie within a factor of two);
+    its own mean is a sum of values of the size of mean|x - mean| + that error, and off by c U of it; the variance by c U of
+    var + error^2 and twice the product of the two errors."""
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    for t, value, step in ((torch.float16, 60000.0, 32.0), (torch.float16, -1500.0, 1.0), (torch.bfloat16, 60160.0, 256.0)):
+        x = torch.full((4, N), value, device="cuda")
+        for m, k in enumerate((1, 3, N // 10, N // 2)):
+            x[m, torch.randperm(N, generator=gen, device="cuda")[:k]] += step
+        x = x.to(t)
+        want, m64, r64, _, _ = reference(x, None, None, 1e-5)
+        x64 = x.double()
+        off = (x64 - m64[:, None]).abs()
+        for y, mean, rstd, c in both_boundaries(x, None, None, aligned):
+            first = c * U * x64.abs().mean(1)
+            second = c * U * (off.mean(1) + first)                      # error of x - mean, beside its own rounding
+            d_rstd = 0.5 * (c + 4) * U * (1 + 2 * (first * r64).square()) + first * second * r64.square() + 4 * U
+            fp32 = ((off * r64[:, None]) * (d_rstd + 4 * U)[:, None] + (second * r64)[:, None])
+            bound = half_step(t) * (want.abs() + fp32) + fp32 + tiny(t)
+            assert ((y.double() - want).abs() / bound).max().item() <= 1.0
+            assert bool(((rstd.double() - r64).abs() <= d_rstd * r64).all())
+            assert bool(((mean.double() - m64).abs() <= second + U * m64.abs()).all())
