@@ -310,7 +310,7 @@ int tw_dense_gemm_bias_act_add(const void* A, int lda, const void* B, int ldb, c
  * they vary by whatever the size of their values (a constant row gives beta); `mean` receives it rounded to fp32.  Non-finite values stay
  * within their row.
  * M >= 0 (M = 0 enqueues nothing).  One kernel, no workspace; it can be recorded into a HIP graph.
- * Errors: TW_ERR_ARG (null X or Y, negative M, N <= 0, pitch too small, unknown dt, eps), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED
+ * Errors: TW_ERR_ARG (null X or Y, negative M, N <= 0, pitch too small, Y = X with another pitch, unknown dt, eps), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED
  * (N above 2^24 - 256; tw_layernorm_t also M above 2^27 - 64), TW_ERR_HIP. */
 int tw_layernorm(const void* X, int ldx, int M, int N, const void* gamma, const void* beta, float eps, void* Y, int ldy,
                  float* mean, float* rstd, tw_dtype dt, void* hip_stream);
@@ -332,7 +332,7 @@ int tw_layernorm_t(const void* Xt, int ldxt, int M, int N, const void* gamma, co
  *                  one each
  * Sums are fp32; those over rows are added in a fixed order (no atomics), so repeated calls give the same bits.  Kernels only, so
  * the call can be recorded into a HIP graph.  M = 0 leaves zeros in dgamma and dbeta.
- * Errors: as tw_layernorm, and TW_ERR_BUF for a workspace that is too small. */
+ * Errors: as tw_layernorm (dX = dY or X with another pitch: TW_ERR_ARG), and TW_ERR_BUF for a workspace that is too small. */
 int tw_layernorm_grad_workspace(int M, int N, size_t* ws_bytes);
 int tw_layernorm_grad(const void* dY, int lddy, const void* X, int ldx, int M, int N, const void* gamma, const float* mean,
                       const float* rstd, void* dX, int lddx, float* dgamma, float* dbeta, void* workspace, size_t ws_bytes,
@@ -357,7 +357,7 @@ int tw_layernorm_grad(const void* dY, int lddy, const void* X, int ldx, int M, i
  * does not see leaves it untouched, whatever its values; non-finite scores or values that it sees give what the formula gives in
  * fp32 (a weight that underflows to zero beside an infinite value: NaN or that infinity).
  * M >= 0 (M = 0 enqueues nothing).  One kernel, no workspace; it can be recorded into a HIP graph (the lengths are read when it runs).
- * Errors: TW_ERR_ARG (null pointer, negative M or n_seqs, heads not a multiple of kv_heads, pitch too small, scale, unknown dt, no
+ * Errors: TW_ERR_ARG (null pointer, negative M or n_seqs, heads not a multiple of kv_heads, pitch too small, O = Q with another pitch, scale, unknown dt, no
  * seq_start and n_seqs > 1), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED (head_dim; ldk or ldv of 2^24 and more; heads * ceil(M / 128) of 2^24
  * and more; a scale above 2.3e38), TW_ERR_HIP. */
 int tw_attention(const void* Q, int ldq, const void* K, int ldk, const void* V, int ldv, void* O, int ldo, int M,

@@ -746,11 +746,16 @@ const void* pick_t(int N) {
 bool odd(const void* q) { return ((uintptr_t)q & 1) != 0; }
 bool vec16(const void* q) { return ((uintptr_t)q & 15) == 0; }
 
+// A result that starts where an operand does is that operand only with the same pitch: else its rows lie over rows that are still to be read.
+bool over_other_rows(const void* out, int ld_out, const void* in, int ld_in, int rows) { return out == in && ld_out != ld_in && rows > 1; }
+
+// (rows, inner: how many rows the matrices have and the elements of one)
 int check_forward(const void* X, int ldx, int M, int N, const void* gamma, const void* beta, float eps, const void* Y, int ldy,
-                  const float* mean, const float* rstd, tw_dtype dt, int inner) {
+                  const float* mean, const float* rstd, tw_dtype dt, int rows, int inner) {
     if ((M > 0 && (!X || !Y)) || M < 0 || N <= 0 || ldx < inner || ldy < inner) return TW_ERR_ARG;
     if (dt != TW_F16 && dt != TW_BF16) return TW_ERR_ARG;
     if (!(eps >= 0.f) || std::isinf(eps)) return TW_ERR_ARG;
+    if (M > 0 && over_other_rows(Y, ldy, X, ldx, rows)) return TW_ERR_ARG;
     if (N > kMaxFeatures) return TW_ERR_UNSUPPORTED;
     if (odd(X) || odd(Y) || odd(gamma) || odd(beta) || ((uintptr_t)mean & 3) != 0 || ((uintptr_t)rstd & 3) != 0) return TW_ERR_ALIGN;
     return TW_OK;
@@ -771,7 +776,7 @@ int grad_parts(int M) {
 
 extern "C" int tw_layernorm(const void* X, int ldx, int M, int N, const void* gamma, const void* beta, float eps, void* Y, int ldy,
                             float* mean, float* rstd, tw_dtype dt, void* hip_stream) {
-    const int rc = check_forward(X, ldx, M, N, gamma, beta, eps, Y, ldy, mean, rstd, dt, N);
+    const int rc = check_forward(X, ldx, M, N, gamma, beta, eps, Y, ldy, mean, rstd, dt, M, N);
     if (rc) return rc;
     if (M == 0) return TW_OK;
     LnParams p{(const us*)X, (const us*)gamma, (const us*)beta, (us*)Y, mean, rstd, ldx, ldy, M, N, eps, 0};
@@ -787,7 +792,7 @@ extern "C" int tw_layernorm(const void* X, int ldx, int M, int N, const void* ga
 
 extern "C" int tw_layernorm_t(const void* Xt, int ldxt, int M, int N, const void* gamma, const void* beta, float eps, void* Yt, int ldyt,
                               float* mean, float* rstd, tw_dtype dt, void* hip_stream) {
-    const int rc = check_forward(Xt, ldxt, M, N, gamma, beta, eps, Yt, ldyt, mean, rstd, dt, M);
+    const int rc = check_forward(Xt, ldxt, M, N, gamma, beta, eps, Yt, ldyt, mean, rstd, dt, N, M);
     if (rc) return rc;
     if (M == 0) return TW_OK;
     LnParams p{(const us*)Xt, (const us*)gamma, (const us*)beta, (us*)Yt, mean, rstd, ldxt, ldyt, M, N, eps,
@@ -812,6 +817,7 @@ extern "C" int tw_layernorm_grad(const void* dY, int lddy, const void* X, int ld
     if ((M > 0 && (!dY || !X || !mean || !rstd || !dX || !workspace)) || M < 0 || N <= 0) return TW_ERR_ARG;
     if (dt != TW_F16 && dt != TW_BF16) return TW_ERR_ARG;
     if (lddy < N || ldx < N || lddx < N) return TW_ERR_ARG;
+    if (over_other_rows(dX, lddx, dY, lddy, M) || over_other_rows(dX, lddx, X, ldx, M)) return TW_ERR_ARG;
     if (N > kMaxFeatures) return TW_ERR_UNSUPPORTED;
     if (odd(dY) || odd(X) || odd(dX) || odd(gamma)) return TW_ERR_ALIGN;
     if ((((uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)dgamma | (uintptr_t)dbeta) & 3) != 0 || !vec16(workspace)) return TW_ERR_ALIGN;

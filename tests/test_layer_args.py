@@ -132,3 +132,17 @@ def test_sizes_beyond_32_bits_are_not_cut():
         with pytest.raises(AssertionError):
             tw._matrix(Operand(rows, cols, ld), rows, cols, Operand(rows, cols, ld))
     assert tw._matrix(Operand(4, 8, 2 ** 31 - 8), 4, 8, Operand(4, 8, 8)) == 2 ** 31 - 8
+
+
+def test_in_place_means_the_same_pitch():
+    """A result that starts where an operand does and has another pitch would be written over rows that are still to be read."""
+    assert ln(ldy=72) == ARG and ln(ld=72) == ARG
+    assert ln("tw_layernorm_t", M=64, N=4, ldy=72) == ARG and ln("tw_layernorm_t", M=64, N=4, ld=128) == ARG
+    other = dict(X=2 * P, dX=3 * P)
+    assert grad(lddx=72) == ARG and grad(lddy=72, X=2 * P) == ARG and grad(ldx=128, dY=2 * P) == ARG
+    assert grad(lddx=72, **{**other, "dX": P}) == ARG and grad(lddx=72, dY=2 * P) == ARG
+    assert attention(O=P, ldo=136) == ARG and attention(Q=P, ldq=256) == ARG
+    # one row has no pitch, no row nothing to write
+    for call in (lambda **kw: ln(ldy=72, **kw), lambda **kw: grad(lddx=72, **kw), lambda **kw: attention(ldo=136, **kw)):
+        assert call(M=1) != ARG and call(M=0) == 0
+    assert ln("tw_layernorm_t", M=64, N=1, ldy=72) != ARG and ln("tw_layernorm_t", M=0, N=4, ldy=72) == 0
