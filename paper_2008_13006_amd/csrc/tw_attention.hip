@@ -436,10 +436,10 @@ extern "C" int tw_attention(const void* Q, int ldq, const void* K, int ldk, cons
     if (heads % kv_heads != 0 || !(scale >= 0.f) || std::isinf(scale)) return TW_ERR_ARG;
     if (!seq_start && n_seqs > 1) return TW_ERR_ARG;
     if ((long)ldq < (long)heads * head_dim || (long)ldo < (long)heads * head_dim || (long)ldk < (long)kv_heads * head_dim || (long)ldv < (long)kv_heads * head_dim) return TW_ERR_ARG;
-    if (O == Q && ldo != ldq && M > 1) return TW_ERR_ARG;    // (O's rows would lie over rows of Q that are still to be read)
     if (head_dim > 128 || (head_dim & 7) != 0 || std::isinf(scale * kLog2e)) return TW_ERR_UNSUPPORTED;
     if (((ldq | ldk | ldv | ldo) & 7) != 0) return TW_ERR_ALIGN;
     if ((((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O) & 15) != 0 || ((uintptr_t)seq_start & 3) != 0) return TW_ERR_ALIGN;
+    if (O == Q && ldo != ldq && M > 1) return TW_ERR_ARG;    // (O's rows would lie over rows of Q that are still to be read)
     // a tile's rows are addressed by 31-bit offsets; a launch holds fewer than 2^32 threads
     if (ldk >= (1 << 24) || ldv >= (1 << 24)) return TW_ERR_UNSUPPORTED;
     const long n_tiles = ((long)M + kRowsPerTile - 1) / kRowsPerTile;
