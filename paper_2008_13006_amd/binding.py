@@ -240,6 +240,18 @@ def _stream_ptr(stream=None) -> int:
     return stream.cuda_stream
 
 
+def _empty(shape, like, stream, dtype=None):
+    """Uninitialised memory that a call allocates beside `like`: an output or scratch.  It is allocated on the stream that uses it, so
+    that it comes from that stream's pool, where nothing of the current stream's is still at work, and goes back there.  (Another stream that
+    is to read an output has to wait for this one, as for any result.)"""
+    torch = _torch()
+    dtype = like.dtype if dtype is None else dtype
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
 def tw_gemm_workspace(blob: np.ndarray, M: int) -> int:
     n = ctypes.c_size_t(0)
     _check(_lib.tw_gemm_workspace(_np_ptr(blob), int(M), ctypes.byref(n)), "tw_gemm_workspace")
@@ -297,8 +309,9 @@ class TwWeight:
         other.ws_limit, other._retired, other._ws_need = self.ws_limit, [], {}
         return other
 
-    def workspace_for(self, M: int):
-        """(pointer, bytes) of a zero-initialised workspace of the size the library wants for M rows."""
+    def workspace_for(self, M: int, stream=None):
+        """(pointer, bytes) of a zero-initialised workspace of the size the library wants for M rows; one that has to grow is allocated and
+        zeroed on `stream` (None: the current one), where the call that asks for it runs."""
         need = self._ws_need.get(M)
         if need is None:
             need = self._ws_need[M] = max(256, tw_gemm_workspace(self.blob, M))
@@ -307,7 +320,8 @@ class TwWeight:
         if need > self.workspace.numel():
             torch = _torch()
             self._retired.append(self.workspace)
-            self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.workspace.device)
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.workspace.device)
         return self.workspace.data_ptr(), need
 
     @classmethod
@@ -330,11 +344,11 @@ def tw_gemm(w: TwWeight, A, C=None, stream=None):
     """C = A . (B * mask).  A: torch tensor [M, K] (f16/bf16, cuda, unit column stride)."""
     M, N = _row_operands(w, A, C)
     if C is None:
-        C = _torch().empty((M, N), dtype=A.dtype, device=A.device)
+        C = _empty((M, N), A, stream)
     lda, ldc = A.stride(0), C.stride(0)
     if M <= 1:
         lda, ldc = max(w.info["K"], lda), max(N, ldc)
-    ws, ws_bytes = w.workspace_for(M)
+    ws, ws_bytes = w.workspace_for(M, stream)
     _check(_lib.tw_gemm(w._blob_ptr, w.blob_dev.data_ptr(), A.data_ptr(),
                         M, lda, C.data_ptr(), ldc, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm")
     return C
@@ -359,14 +373,13 @@ def tw_gemm_t(w: TwWeight, At, Ct=None, stream=None):
 
 def tw_gemm_t_bias_act(w: TwWeight, At, bias=None, act="none", Ct=None, stream=None):
     """Ct = act(A . (B * mask) + bias)^T from At = A^T; bias: torch tensor [N] or None."""
-    torch = _torch()
     assert At.is_cuda and At.dtype == w.torch_dtype and At.dim() == 2 and At.stride(1) == 1
     K, M = At.shape
     assert K == w.info["K"]
     N = w.info["N"]
     if Ct is None:
         ld = (M + 63) // 64 * 64
-        Ct = torch.empty((N, ld), dtype=At.dtype, device=At.device)[:, :M]
+        Ct = _empty((N, ld), At, stream)[:, :M]
     assert Ct.is_cuda and Ct.dtype == At.dtype and Ct.shape == (N, M) and Ct.stride(1) == 1
     ldat = At.stride(0) if K > 1 else max(M, At.stride(0))
     ldct = Ct.stride(0) if N > 1 else max(M, Ct.stride(0))
@@ -374,7 +387,7 @@ def tw_gemm_t_bias_act(w: TwWeight, At, bias=None, act="none", Ct=None, stream=N
     if bias is not None:
         assert bias.is_cuda and bias.dtype == At.dtype and bias.shape == (N,) and bias.stride(0) == 1
         bptr = bias.data_ptr()
-    ws, ws_bytes = w.workspace_for(M)
+    ws, ws_bytes = w.workspace_for(M, stream)
     if bias is None and _act_code(act) == TW_ACT_NONE:
         _check(_lib.tw_gemm_t(w._blob_ptr, w.blob_dev.data_ptr(), At.data_ptr(),
                               M, ldat, Ct.data_ptr(), ldct, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm_t")
@@ -388,12 +401,11 @@ def tw_gemm_t_bias_act(w: TwWeight, At, bias=None, act="none", Ct=None, stream=N
 
 def tw_transpose(src, dst=None, stream=None):
     """dst = src^T for a 2-D torch tensor of a 16-bit type (unit column stride)."""
-    torch = _torch()
     assert src.is_cuda and src.dim() == 2 and src.stride(1) == 1 and src.element_size() == 2
     rows, cols = src.shape
     if dst is None:
         ld = (rows + 63) // 64 * 64
-        dst = torch.empty((cols, ld), dtype=src.dtype, device=src.device)[:, :rows]
+        dst = _empty((cols, ld), src, stream)[:, :rows]
     assert dst.shape == (cols, rows) and dst.dtype == src.dtype and dst.stride(1) == 1
     lds = src.stride(0) if rows > 1 else max(cols, src.stride(0))
     ldd = dst.stride(0) if cols > 1 else max(rows, dst.stride(0))
@@ -414,7 +426,7 @@ def tw_gemm_bias_act(w: TwWeight, A, bias=None, act="none", C=None, stream=None)
     """C = act(A . (B * mask) + bias).  bias: torch tensor [N] of A's dtype on the GPU, or None."""
     M, N = _row_operands(w, A, C)
     if C is None:
-        C = _torch().empty((M, N), dtype=A.dtype, device=A.device)
+        C = _empty((M, N), A, stream)
     bptr = None
     if bias is not None:
         assert bias.is_cuda and bias.dtype == A.dtype and bias.shape == (N,) and bias.stride(0) == 1
@@ -422,7 +434,7 @@ def tw_gemm_bias_act(w: TwWeight, A, bias=None, act="none", C=None, stream=None)
     lda, ldc = A.stride(0), C.stride(0)
     if M <= 1:
         lda, ldc = max(w.info["K"], lda), max(N, ldc)
-    ws, ws_bytes = w.workspace_for(M)
+    ws, ws_bytes = w.workspace_for(M, stream)
     _check(_lib.tw_gemm_bias_act(w._blob_ptr, w.blob_dev.data_ptr(),
                                  A.data_ptr(), M, lda, bptr, _act_code(act),
                                  C.data_ptr(), ldc, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm_bias_act")
@@ -438,7 +450,7 @@ def tw_dense_gemm_bias_act(A, B, bias=None, act="none", C=None, stream=None):
     K2, N = B.shape
     assert K == K2
     if C is None:
-        C = torch.empty((M, N), dtype=A.dtype, device=A.device)
+        C = _empty((M, N), A, stream)
     assert C.shape == (M, N) and C.dtype == A.dtype and C.stride(1) == 1
     bptr = None
     if bias is not None:
@@ -463,7 +475,7 @@ def tw_dense_gemm(A, B, C=None, stream=None):
     K2, N = B.shape
     assert K == K2
     if C is None:
-        C = torch.empty((M, N), dtype=A.dtype, device=A.device)
+        C = _empty((M, N), A, stream)
     assert C.shape == (M, N) and C.dtype == A.dtype and C.stride(1) == 1
     dt = TW_F16 if A.dtype == torch.float16 else TW_BF16
     lda = A.stride(0) if M > 1 else max(K, A.stride(0))
@@ -509,22 +521,22 @@ def _vector(t, n, dtype, like):
     return t.data_ptr()
 
 
-def _new_matrix(rows, cols, like):
+def _new_matrix(rows, cols, like, stream):
     """An output of the pitch that the kernels take 16 bytes at a time."""
-    return _torch().empty((rows, -(-cols // 8) * 8), dtype=like.dtype, device=like.device)[:, :cols]
+    return _empty((rows, -(-cols // 8) * 8), like, stream)[:, :cols]
 
 
 def tw_gemm_bias_act_add(w: TwWeight, A, R, bias=None, act="none", C=None, stream=None):
     """C = act(A . (B * mask) + bias) + R.  R: torch tensor [M, N] of A's type; C may be R (see include/tw.h)."""
     M, N = _row_operands(w, A, C)
     if C is None:
-        C = _torch().empty((M, N), dtype=A.dtype, device=A.device)
+        C = _empty((M, N), A, stream)
     ldr = _matrix(R, M, N, A)
     b = _vector(bias, N, A.dtype, A)
     lda, ldc = A.stride(0), C.stride(0)
     if M <= 1:
         lda, ldc = max(w.info["K"], lda), N
-    ws, ws_bytes = w.workspace_for(M)
+    ws, ws_bytes = w.workspace_for(M, stream)
     _check(_lib.tw_gemm_bias_act_add(w._blob_ptr, w.blob_dev.data_ptr(), A.data_ptr(), M, lda, b, _act_code(act), R.data_ptr(), ldr,
                                      C.data_ptr(), ldc, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm_bias_act_add")
     return C
@@ -536,10 +548,10 @@ def tw_gemm_t_bias_act_add(w: TwWeight, At, Rt, bias=None, act="none", Ct=None, 
     K, M = At.shape
     N = w.info["N"]
     if Ct is None:
-        Ct = _torch().empty((N, (M + 63) // 64 * 64), dtype=At.dtype, device=At.device)[:, :M]
+        Ct = _empty((N, (M + 63) // 64 * 64), At, stream)[:, :M]
     ldat, ldrt, ldct = _matrix8(At, K, M, At), _matrix8(Rt, N, M, At), _matrix8(Ct, N, M, At)
     b = _vector(bias, N, At.dtype, At)
-    ws, ws_bytes = w.workspace_for(M)
+    ws, ws_bytes = w.workspace_for(M, stream)
     _check(_lib.tw_gemm_t_bias_act_add(w._blob_ptr, w.blob_dev.data_ptr(), At.data_ptr(), M, ldat, b, _act_code(act), Rt.data_ptr(), ldrt,
                                        Ct.data_ptr(), ldct, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm_t_bias_act_add")
     return Ct
@@ -552,7 +564,7 @@ def tw_dense_gemm_bias_act_add(A, B, R, bias=None, act="none", C=None, stream=No
     M, K = A.shape
     N = B.shape[1]
     if C is None:
-        C = _new_matrix(M, N, A)
+        C = _new_matrix(M, N, A, stream)
     lda, ldb, ldr, ldc = _matrix8(A, M, K, A), _matrix8(B, K, N, A), _matrix8(R, M, N, A), _matrix8(C, M, N, A)
     b = _vector(bias, N, A.dtype, A)
     _check(_lib.tw_dense_gemm_bias_act_add(A.data_ptr(), lda, B.data_ptr(), ldb, b, _act_code(act), R.data_ptr(), ldr, C.data_ptr(), ldc,
@@ -564,7 +576,7 @@ def _layernorm(entry, where, X, M, N, gamma, beta, eps, Y, mean, rstd, stream):
     assert X.is_cuda and X.dim() == 2
     dt = _dt_code(X)
     if Y is None:
-        Y = _new_matrix(*X.shape, X)
+        Y = _new_matrix(*X.shape, X, stream)
     rows, cols = X.shape
     ldx, ldy = _matrix(X, rows, cols, X), _matrix(Y, rows, cols, X)
     g, b = _vector(gamma, N, X.dtype, X), _vector(beta, N, X.dtype, X)
@@ -601,15 +613,13 @@ def tw_layernorm_grad(dY, X, gamma, mean, rstd, dX=None, dgamma=None, dbeta=None
     M, N = X.shape
     dt = _dt_code(X)
     if workspace is None:
-        # (allocated on the stream that uses it: its memory goes back to that stream's pool)
-        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-            workspace = torch.empty(tw_layernorm_grad_workspace(M, N), dtype=torch.uint8, device=X.device)
+        workspace = _empty(tw_layernorm_grad_workspace(M, N), X, stream, torch.uint8)
     if dX is None:
-        dX = _new_matrix(M, N, X)
+        dX = _new_matrix(M, N, X, stream)
     if dgamma is None:
-        dgamma = torch.empty(N, dtype=torch.float32, device=X.device)
+        dgamma = _empty(N, X, stream, torch.float32)
     if dbeta is None:
-        dbeta = torch.empty(N, dtype=torch.float32, device=X.device)
+        dbeta = _empty(N, X, stream, torch.float32)
     assert workspace.is_cuda and workspace.get_device() == X.get_device() and workspace.dtype == torch.uint8 and workspace.is_contiguous()
     lddy, ldx, lddx = _matrix(dY, M, N, X), _matrix(X, M, N, X), _matrix(dX, M, N, X)
     g = _vector(gamma, N, X.dtype, X)
@@ -630,7 +640,7 @@ def tw_attention(Q, K, V, seq_start, heads: int, kv_heads: Optional[int] = None,
     M, d = Q.shape[0], Q.shape[1] // heads
     dt = _dt_code(Q)
     if O is None:
-        O = _new_matrix(M, heads * d, Q)
+        O = _new_matrix(M, heads * d, Q, stream)
     ldq, ldo = _matrix8(Q, M, heads * d, Q), _matrix8(O, M, heads * d, Q)
     ldk, ldv = _matrix8(K, M, kv_heads * d, Q), _matrix8(V, M, kv_heads * d, Q)
     n_seqs, starts = 0, None

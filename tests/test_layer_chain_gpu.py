@@ -160,3 +160,50 @@ def test_norm_of_a_step(tw):
         torch.cuda.synchronize()
         check_forward(layer.out, layer.mean, layer.rstd, layer.sum2, layer.gamma[1], layer.beta[1], 1e-5)
         check_grad(dx, dgamma, dbeta, dy, layer.sum2, layer.gamma[1], layer.mean, layer.rstd)
+
+
+CALLS = {
+    "gemm": lambda tw, o, w, s: tw.tw_gemm(w, o["a"], stream=s),
+    "gemm_t": lambda tw, o, w, s: tw.tw_gemm_t(w, o["at"], stream=s),
+    "gemm_bias_act": lambda tw, o, w, s: tw.tw_gemm_bias_act(w, o["a"], act="relu", stream=s),
+    "transpose": lambda tw, o, w, s: tw.tw_transpose(o["a"], stream=s),
+    "dense": lambda tw, o, w, s: tw.tw_dense_gemm(o["a"], o["b"], stream=s),
+    "dense_bias_act": lambda tw, o, w, s: tw.tw_dense_gemm_bias_act(o["a"], o["b"], stream=s),
+    "gemm_add": lambda tw, o, w, s: tw.tw_gemm_bias_act_add(w, o["a"], o["r"], stream=s),
+    "gemm_t_add": lambda tw, o, w, s: tw.tw_gemm_t_bias_act_add(w, o["at"], o["rt"], stream=s),
+    "dense_add": lambda tw, o, w, s: tw.tw_dense_gemm_bias_act_add(o["a"], o["b"], o["r"], stream=s),
+    "layernorm": lambda tw, o, w, s: tw.tw_layernorm(o["r"], stream=s),
+    "layernorm_t": lambda tw, o, w, s: tw.tw_layernorm_t(o["rt"], stream=s),
+    "layernorm_grad": lambda tw, o, w, s: tw.tw_layernorm_grad(o["r"], o["r"], None, o["mean"], o["rstd"], stream=s),
+    "attention": lambda tw, o, w, s: tw.tw_attention(o["r"][:, :64], o["r"][:, 64:128], o["r"][:, 128:192], None, 1, stream=s),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_what_a_call_allocates_belongs_to_its_stream(tw, name):
+    """With `stream`, outputs that are not given and a workspace that grows come from that stream's memory, not from the current one's,
+    whose last user may still be running; what comes back is what the call on the current stream gives."""
+    t, M, K, N = torch.float16, 64, 2048, 256
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    spec = W.small_spec("streams", M=1, K=K, N=N, G=64, dtype="f16", col_prune=0.05, keep=("upow", 0.1, 0.5), seed_offset=9400)
+    w = W.generate(spec)
+    blob = tw.tw_pack(w.B, w.mask, 64, "f16")
+    assert tw.tw_gemm_workspace(blob, M) > 256                   # (K is split: the products let their workspaces grow)
+    o = {k: torch.randn(s, generator=gen, device="cuda").to(t) for k, s in (("a", (M, K)), ("r", (M, N)), ("b", (K, N)))}
+    o.update(at=o["a"].t().contiguous(), rt=o["r"].t().contiguous(), mean=torch.zeros(M, device="cuda"), rstd=torch.ones(M, device="cuda"))
+
+    def stream_of(x):
+        at = x.data_ptr()
+        return next(seg["stream"] for seg in torch.cuda.memory_snapshot() if seg["address"] <= at < seg["address"] + seg["total_size"])
+
+    want = CALLS[name](tw, o, tw.TwWeight(blob), None)
+    fresh = tw.TwWeight(blob)
+    held = fresh.workspace
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = CALLS[name](tw, o, fresh, side)
+    torch.cuda.current_stream().wait_stream(side)
+    for x, y in zip(got, want) if isinstance(got, tuple) else [(got, want)]:
+        assert stream_of(x) == side.cuda_stream and torch.equal(x, y)
+    assert fresh.workspace is held or stream_of(fresh.workspace) == side.cuda_stream
+    side.synchronize()
