@@ -521,9 +521,9 @@ def _vector(t, n, dtype, like):
     return t.data_ptr()
 
 
-def _new_matrix(rows, cols, like, stream):
-    """An output of the pitch that the kernels take 16 bytes at a time."""
-    return _empty((rows, -(-cols // 8) * 8), like, stream)[:, :cols]
+def _new_matrix(rows, cols, like, stream, multiple=8):
+    """An output of the pitch that the kernels take 16 bytes at a time (multiple = 64: whose rows start 128-byte lines)."""
+    return _empty((rows, -(-cols // multiple) * multiple), like, stream)[:, :cols]
 
 
 def tw_gemm_bias_act_add(w: TwWeight, A, R, bias=None, act="none", C=None, stream=None):
@@ -572,11 +572,11 @@ def tw_dense_gemm_bias_act_add(A, B, R, bias=None, act="none", C=None, stream=No
     return C
 
 
-def _layernorm(entry, where, X, M, N, gamma, beta, eps, Y, mean, rstd, stream):
+def _layernorm(entry, where, X, M, N, gamma, beta, eps, Y, mean, rstd, stream, multiple):
     assert X.is_cuda and X.dim() == 2
     dt = _dt_code(X)
     if Y is None:
-        Y = _new_matrix(*X.shape, X, stream)
+        Y = _new_matrix(*X.shape, X, stream, multiple)
     rows, cols = X.shape
     ldx, ldy = _matrix(X, rows, cols, X), _matrix(Y, rows, cols, X)
     g, b = _vector(gamma, N, X.dtype, X), _vector(beta, N, X.dtype, X)
@@ -591,12 +591,12 @@ def _layernorm(entry, where, X, M, N, gamma, beta, eps, Y, mean, rstd, stream):
 def tw_layernorm(X, gamma=None, beta=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
     """Layer norm of every row of X [M, N]; gamma, beta: [N] of X's type or None.  mean, rstd: float32 [M] to be filled
     for a backward pass, or None.  Y may be X."""
-    return _layernorm(_lib.tw_layernorm, "tw_layernorm", X, X.shape[0], X.shape[1], gamma, beta, eps, Y, mean, rstd, stream)
+    return _layernorm(_lib.tw_layernorm, "tw_layernorm", X, X.shape[0], X.shape[1], gamma, beta, eps, Y, mean, rstd, stream, 8)
 
 
 def tw_layernorm_t(Xt, gamma=None, beta=None, eps=1e-5, Yt=None, mean=None, rstd=None, stream=None):
     """Layer norm of every COLUMN of Xt [N, M] (the transposed boundary: a row per feature); gamma, beta: [N] or None."""
-    return _layernorm(_lib.tw_layernorm_t, "tw_layernorm_t", Xt, Xt.shape[1], Xt.shape[0], gamma, beta, eps, Yt, mean, rstd, stream)
+    return _layernorm(_lib.tw_layernorm_t, "tw_layernorm_t", Xt, Xt.shape[1], Xt.shape[0], gamma, beta, eps, Yt, mean, rstd, stream, 64)
 
 
 def tw_layernorm_grad_workspace(M: int, N: int) -> int:

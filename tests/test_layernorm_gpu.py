@@ -349,3 +349,13 @@ def test_rows_that_hardly_vary(N, aligned):
             assert ((y.double() - want).abs() / bound).max().item() <= 1.0
             assert bool(((rstd.double() - r64).abs() <= d_rstd * r64).all())
             assert bool(((mean.double() - m64).abs() <= second + U * m64.abs()).all())
+
+
+def test_rows_of_a_default_output_start_lines():
+    """What tw_layernorm_t allocates has the pitch that whole lines are stored with; what it leaves is what an output of another pitch gets."""
+    for M in (8, 63, 64, 200):
+        xt = torch.randn((96, M), device="cuda").to(torch.float16)
+        yt = tw.tw_layernorm_t(xt)
+        assert yt.shape == (96, M) and yt.stride(1) == 1 and yt.stride(0) == -(-M // 64) * 64 and yt.data_ptr() % 128 == 0
+        other, _ = make(96, M, torch.float16)
+        assert torch.equal(tw.tw_layernorm_t(xt, Yt=other), yt)
