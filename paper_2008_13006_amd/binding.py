@@ -229,15 +229,33 @@ def _tdtype(dtype: str):
     return torch.float16 if dtype == "f16" else torch.bfloat16
 
 
+def _current_device() -> int:
+    torch = _torch()
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:          # (names of torch's own that a version may lack)
+        return torch.cuda.current_device()
+
+
+def _raw_stream(device=None) -> int:
+    # (the raw handle of the current stream of the current device, without building a torch Stream object for it)
+    torch = _torch()
+    try:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice() if device is None else device)
+    except AttributeError:          # (likewise)
+        return torch.cuda.current_stream().cuda_stream
+
+
 def _stream_ptr(stream=None) -> int:
-    # (the raw handle of the current device's current stream, without building a torch Stream object for it)
-    if stream is None:
-        torch = _torch()
-        try:
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-        except AttributeError:      # (names of torch's own that a version may lack)
-            return torch.cuda.current_stream().cuda_stream
-    return stream.cuda_stream
+    return _raw_stream() if stream is None else stream.cuda_stream
+
+
+def _launch_stream(like, stream) -> int:
+    """The raw handle of `stream` (None: the current one) for a call whose operands lie beside `like`: the library launches on the current device,
+    so they and the stream have to be of it."""
+    device = _current_device()
+    assert like.get_device() == device and (stream is None or stream.device_index == device), "operands and stream have to be of the current device"
+    return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
 def _empty(shape, like, stream, dtype=None):
@@ -538,7 +556,7 @@ def tw_gemm_bias_act_add(w: TwWeight, A, R, bias=None, act="none", C=None, strea
         lda, ldc = max(w.info["K"], lda), N
     ws, ws_bytes = w.workspace_for(M, stream)
     _check(_lib.tw_gemm_bias_act_add(w._blob_ptr, w.blob_dev.data_ptr(), A.data_ptr(), M, lda, b, _act_code(act), R.data_ptr(), ldr,
-                                     C.data_ptr(), ldc, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm_bias_act_add")
+                                     C.data_ptr(), ldc, ws, ws_bytes, _launch_stream(A, stream)), "tw_gemm_bias_act_add")
     return C
 
 
@@ -553,7 +571,7 @@ def tw_gemm_t_bias_act_add(w: TwWeight, At, Rt, bias=None, act="none", Ct=None, 
     b = _vector(bias, N, At.dtype, At)
     ws, ws_bytes = w.workspace_for(M, stream)
     _check(_lib.tw_gemm_t_bias_act_add(w._blob_ptr, w.blob_dev.data_ptr(), At.data_ptr(), M, ldat, b, _act_code(act), Rt.data_ptr(), ldrt,
-                                       Ct.data_ptr(), ldct, ws, ws_bytes, _stream_ptr(stream)), "tw_gemm_t_bias_act_add")
+                                       Ct.data_ptr(), ldct, ws, ws_bytes, _launch_stream(At, stream)), "tw_gemm_t_bias_act_add")
     return Ct
 
 
@@ -568,7 +586,7 @@ def tw_dense_gemm_bias_act_add(A, B, R, bias=None, act="none", C=None, stream=No
     lda, ldb, ldr, ldc = _matrix8(A, M, K, A), _matrix8(B, K, N, A), _matrix8(R, M, N, A), _matrix8(C, M, N, A)
     b = _vector(bias, N, A.dtype, A)
     _check(_lib.tw_dense_gemm_bias_act_add(A.data_ptr(), lda, B.data_ptr(), ldb, b, _act_code(act), R.data_ptr(), ldr, C.data_ptr(), ldc,
-                                           M, N, K, dt, _stream_ptr(stream)), "tw_dense_gemm_bias_act_add")
+                                           M, N, K, dt, _launch_stream(A, stream)), "tw_dense_gemm_bias_act_add")
     return C
 
 
@@ -584,7 +602,7 @@ def _layernorm(entry, where, X, M, N, gamma, beta, eps, Y, mean, rstd, stream, m
     if mean is not None or rstd is not None:
         f32 = _torch().float32
         mu, rs = _vector(mean, M, f32, X), _vector(rstd, M, f32, X)
-    _check(entry(X.data_ptr(), ldx, M, N, g, b, float(eps), Y.data_ptr(), ldy, mu, rs, dt, _stream_ptr(stream)), where)
+    _check(entry(X.data_ptr(), ldx, M, N, g, b, float(eps), Y.data_ptr(), ldy, mu, rs, dt, _launch_stream(X, stream)), where)
     return Y
 
 
@@ -625,7 +643,7 @@ def tw_layernorm_grad(dY, X, gamma, mean, rstd, dX=None, dgamma=None, dbeta=None
     g = _vector(gamma, N, X.dtype, X)
     f32 = torch.float32
     _check(_lib.tw_layernorm_grad(dY.data_ptr(), lddy, X.data_ptr(), ldx, M, N, g, _vector(mean, M, f32, X), _vector(rstd, M, f32, X), dX.data_ptr(),
-                                  lddx, _vector(dgamma, N, f32, X), _vector(dbeta, N, f32, X), workspace.data_ptr(), workspace.numel(), dt, _stream_ptr(stream)), "tw_layernorm_grad")
+                                  lddx, _vector(dgamma, N, f32, X), _vector(dbeta, N, f32, X), workspace.data_ptr(), workspace.numel(), dt, _launch_stream(X, stream)), "tw_layernorm_grad")
     return dX, dgamma, dbeta
 
 
@@ -649,7 +667,7 @@ def tw_attention(Q, K, V, seq_start, heads: int, kv_heads: Optional[int] = None,
         n_seqs = seq_start.numel() - 1
         starts = _vector(seq_start, n_seqs + 1, torch.int32, Q)
     _check(_lib.tw_attention(Q.data_ptr(), ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, O.data_ptr(), ldo, M, starts, n_seqs, heads, kv_heads, d,
-                             d ** -0.5 if scale is None else float(scale), int(bool(causal)), dt, _stream_ptr(stream)), "tw_attention")
+                             d ** -0.5 if scale is None else float(scale), int(bool(causal)), dt, _launch_stream(Q, stream)), "tw_attention")
     return O
 
 

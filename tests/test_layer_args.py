@@ -146,3 +146,55 @@ def test_in_place_means_the_same_pitch():
     for call in (lambda **kw: ln(ldy=72, **kw), lambda **kw: grad(lddx=72, **kw), lambda **kw: attention(ldo=136, **kw)):
         assert call(M=1) != ARG and call(M=0) == 0
     assert ln("tw_layernorm_t", M=64, N=1, ldy=72) != ARG and ln("tw_layernorm_t", M=0, N=4, ldy=72) == 0
+
+
+def test_operands_and_stream_of_another_device(monkeypatch):
+    """The library launches on the current device: operands or a stream of another one are refused before it is called."""
+    from types import SimpleNamespace
+    import numpy as np
+
+    class Operand:
+        is_cuda = True
+
+        def __init__(self, *shape, dtype=torch.float16):
+            self.shape, self.dtype, self.device = shape, dtype, "cuda:1"
+
+        def get_device(self):
+            return 1
+
+        def dim(self):
+            return len(self.shape)
+
+        def numel(self):
+            return int(np.prod(self.shape))
+
+        def is_contiguous(self):
+            return True
+
+        def stride(self, k=None):
+            steps = (self.shape[1], 1) if len(self.shape) == 2 else (1,)
+            return steps if k is None else steps[k]
+
+        def data_ptr(self):
+            return P
+
+    x, seq, f = Operand(64, 64), Operand(2, dtype=torch.int32), Operand(64, dtype=torch.float32)
+    w = SimpleNamespace(info={"K": 64, "N": 64}, torch_dtype=torch.float16, workspace_for=lambda M, stream=None: (P, 256), _blob_ptr=P, blob_dev=x)
+    calls = [lambda s: tw.tw_gemm_bias_act_add(w, x, x, C=Operand(64, 64), stream=s), lambda s: tw.tw_gemm_t_bias_act_add(w, x, x, Ct=Operand(64, 64), stream=s),
+             lambda s: tw.tw_dense_gemm_bias_act_add(x, x, x, C=x, stream=s), lambda s: tw.tw_layernorm(x, Y=x, stream=s), lambda s: tw.tw_layernorm_t(x, Yt=x, stream=s),
+             lambda s: tw.tw_layernorm_grad(x, x, None, f, f, x, f, f, Operand(1 << 20, dtype=torch.uint8), stream=s), lambda s: tw.tw_attention(x, x, x, seq, 1, O=x, stream=s)]
+    reached = []
+    library = SimpleNamespace(**{name: lambda *args, name=name: reached.append(name) or 0 for name in tw.SYMBOLS})
+    monkeypatch.setattr(tw, "_lib", library)
+    here, there = (SimpleNamespace(cuda_stream=5, device_index=k) for k in (1, 0))
+    for k, call in enumerate(calls):
+        monkeypatch.setattr(tw, "_current_device", lambda: 0)
+        for s in (None, here, there):
+            with pytest.raises(AssertionError, match="current device"):
+                call(s)
+        monkeypatch.setattr(tw, "_current_device", lambda: 1)
+        with pytest.raises(AssertionError, match="current device"):
+            call(there)
+        assert len(reached) == k
+        call(here)
+        assert len(reached) == k + 1
