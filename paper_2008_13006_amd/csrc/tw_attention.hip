@@ -399,6 +399,13 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
         }
     }
     const float inv = 1.f / l;
+    // A mean of values that f16 holds is one itself, but the weights' rounding adds up to half a step of the largest: back to that one, unless
+    // an infinity among the values made it.
+    auto mean = [&](float sum) __attribute__((always_inline)) {
+        const float x = sum * inv;
+        if constexpr (DT == TW_F16) return __builtin_fabsf(x) < __builtin_inff() ? __builtin_fminf(__builtin_fmaxf(x, -65504.f), 65504.f) : x;
+        else return x;
+    };
     __syncthreads();                                         // the staging areas of the results lie over the tiles
     unsigned char* stage = smem + wave * (32 * OPITCH);
 #pragma unroll
@@ -406,8 +413,8 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             tw_u32x2 v;
-            v.x = (unsigned)tw_cvt<DT>(o[f][4 * c] * inv) | ((unsigned)tw_cvt<DT>(o[f][4 * c + 1] * inv) << 16);
-            v.y = (unsigned)tw_cvt<DT>(o[f][4 * c + 2] * inv) | ((unsigned)tw_cvt<DT>(o[f][4 * c + 3] * inv) << 16);
+            v.x = (unsigned)tw_cvt<DT>(mean(o[f][4 * c])) | ((unsigned)tw_cvt<DT>(mean(o[f][4 * c + 1])) << 16);
+            v.y = (unsigned)tw_cvt<DT>(mean(o[f][4 * c + 2])) | ((unsigned)tw_cvt<DT>(mean(o[f][4 * c + 3])) << 16);
             *(tw_u32x2*)(stage + l32 * OPITCH + (32 * f + 8 * c + 4 * h) * 2) = v;
         }
     const unsigned long long rows = __builtin_amdgcn_ballot_w64(valid);      // (both halves alike)

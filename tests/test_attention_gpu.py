@@ -277,3 +277,30 @@ def test_many_tiles_of_different_lengths(heads, d, lens, before, after, causal):
     again = q.clone()
     run(again, k, v, starts, heads, 1, causal, O=again)
     assert torch.equal(again[before:starts[-1]], o[before:starts[-1]]) and torch.equal(again[:before], q[:before])
+
+
+def test_means_of_the_largest_values_stay_finite():
+    """A result is a mean of values: where all are the type's largest it is that value, though the rounding of the weights may add up to half a step."""
+    heads, d = 4, 64
+    starts = starts_of([2, 3, 5, 9, 70, 200])
+    for dtype, t in TYPES.items():
+        big = 65504.0 if t == torch.float16 else 2.0 ** 100
+        q, k, v = make(starts[-1], heads, heads, d, dtype, 33, size=0.7)
+        v[:] = big
+        v[:, ::2] = -big
+        for causal in (False, True):
+            o = run(q, k, v, starts, heads, heads, causal).double()
+            assert bool(torch.isfinite(o).all())
+            assert ((o - v.double()).abs() / big).max().item() <= torch.finfo(t).eps
+        # every weight but one is 0.5 (1 + 2^-11) and a little: rounded up by nearly half a step of f16
+        q2, k2 = torch.zeros_like(q), torch.zeros_like(k)
+        score = torch.tensor(0.5 * (1 + 1.05 * 2.0 ** -11), dtype=torch.float64).log()
+        q2[:, 0::d] = q2[:, 1::d] = 1.0
+        k2[:, 0::d] = score.to(t)
+        k2[:, 1::d] = (score - score.to(t).double()).to(t)
+        k2[torch.tensor(starts[:-1], device="cuda")] = 0.0
+        o = run(q2, k2, v, starts, heads, heads, False, scale=1.0).double()
+        assert bool(torch.isfinite(o).all()) and ((o - v.double()).abs() / big).max().item() <= torch.finfo(t).eps
+        v[4] = float("inf")                                      # an infinity stays one
+        o = run(q, k, v, starts, heads, heads, False)
+        assert bool((o[2:5] == float("inf")).all()) and bool(torch.isfinite(o[:2]).all()) and bool(torch.isfinite(o[5:]).all())
