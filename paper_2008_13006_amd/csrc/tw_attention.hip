@@ -243,6 +243,10 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
     const float scale2 = flat ? 1.f : p.scale2;
     constexpr us kInf = DT == TW_F16 ? 0x7C00 : 0x7F80;
     bool odd = false;                                        // values that are not finite lie beside keys that some row does not see
+    // From 2^20 on a score's product with scale2 is rounded before the reference is taken from it, as it was for the reference: the fused form
+    // would leave that rounding, up to half a step of the product, in the exponent of the largest (2^24 and more: whole powers of two).
+    bool large = false;
+    constexpr float kLarge = 1048576.f;
     // operands are read that many products ahead (d = 128, one prompt of 8192: four 270 us, eight 262; of 64 there are two workgroups more
     // to a compute unit with the registers of four)
     constexpr int kAhead = KS >= 6 ? 8 : 4;
@@ -304,11 +308,12 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
         top = max_halves(top) * scale2;
         // The exponents' reference moves only when some row's maximum has grown by more than kSlack powers of two: the weights stay below
         // 2^kSlack, which 16 bits hold as precisely, and most tiles scale nothing.
-        if (__any(top > ref + kSlack)) {
+        if (__any(top - ref > kSlack)) {                     // (the difference: a step of the sum may be larger than the slack)
             const float next_ref = __builtin_fmaxf(ref, top);
             const float from = ref == -__builtin_inff() ? next_ref : ref;     // (nothing summed yet; -inf twice: no key seen)
             const float fade = __builtin_amdgcn_exp2f(ref == next_ref ? 0.f : from - next_ref);
             ref = next_ref;
+            large |= __any(__builtin_fabsf(ref) > kLarge && __builtin_fabsf(ref) < __builtin_inff()) != 0;
             l *= fade;
 #pragma unroll
             for (int f = 0; f < FB; ++f)
@@ -316,6 +321,15 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
                 for (int r = 0; r < 16; ++r) o[f][r] *= fade;
         }
         const float base = ref == -__builtin_inff() ? 0.f : ref;          // (no key yet, or only scores of -inf: all weights 0)
+        float factor = scale2;
+        if (large) {
+            asm volatile("" : "+v"(factor));                 // (as above)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] *= factor;
+            factor = 1.f;
+        }
         tw_u16x8 w[4];                                       // weights: operand of contraction step 2 b + r / 8
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
         // A request for the next tile, then its share of the exponentials: a compute unit takes 64 bytes of requests a clock, and a wave that makes
@@ -329,7 +343,7 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
                 next(i / kShare);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], scale2, -base));
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], factor, -base));
             sum[r & 3] += e;
             w[2 * b + (r >> 3)][r & 7] = tw_cvt<DT>(e);
         }
@@ -365,9 +379,11 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // nothing on its way into LDS any more
     l += __shfl_xor(l, 32);
-    // Rare: a value that is not finite, beside keys that some row of the wave does not see, has met a weight of zero there.  The sums with V
-    // are made again, key by key, each row's own keys only (maximum and sum of the weights do not depend on V).
+    // Rare: a value that is not finite, beside keys that some row of the wave does not see, has met a weight of zero there.  Everything is made
+    // again, key by key, each row's own keys only.  (Not the sums with V alone: scores of 2^24 and more whose products are added in another
+    // order have other weights than those that l has summed.)
     if (odd) {
+        float most = -__builtin_inff(), weights = 0.f;
 #pragma unroll
         for (int f = 0; f < FB; ++f)
 #pragma unroll
@@ -386,8 +402,19 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
                 }
             x += __shfl_xor(x, 32);
             if (flat) x *= 0.f;
-            const float e = tw_to_f32<DT>(tw_cvt<DT>(__builtin_amdgcn_exp2f(__builtin_fmaf(x, scale2, ref == -__builtin_inff() ? 0.f : -ref))));
             if ((unsigned)(key - lo) >= (unsigned)(hi - lo)) continue;
+            x *= scale2;
+            if (x > most) {
+                const float fade = most == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(most - x);
+                weights *= fade;
+#pragma unroll
+                for (int f = 0; f < FB; ++f)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[f][r] *= fade;
+                most = x;
+            }
+            const float e = __builtin_amdgcn_exp2f(x - (most == -__builtin_inff() ? 0.f : most));
+            weights += e;
 #pragma unroll
             for (int f = 0; f < FB; ++f)
 #pragma unroll
@@ -397,6 +424,7 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
                     o[f][r] += __builtin_fabsf(v) < __builtin_inff() ? e * v : v;
                 }
         }
+        l = weights;
     }
     const float inv = 1.f / l;
     // A mean of values that f16 holds is one itself, but the weights' rounding adds up to half a step of the largest: back to that one, unless

@@ -304,3 +304,37 @@ def test_means_of_the_largest_values_stay_finite():
         v[4] = float("inf")                                      # an infinity stays one
         o = run(q, k, v, starts, heads, heads, False)
         assert bool((o[2:5] == float("inf")).all()) and bool(torch.isfinite(o[:2]).all()) and bool(torch.isfinite(o[5:]).all())
+
+
+def test_scores_beyond_what_a_step_of_fp32_resolves():
+    """Scores of 10^8 to 10^10, where neighbours in fp32 lie 8 to 1024 apart: the largest take everything, equally where they are equal."""
+    n, d = 300, 64
+    for dtype, t in TYPES.items():
+        for unit in (1024.0, 8192.0, 32768.0):
+            q = torch.zeros((n, d), dtype=t, device="cuda")
+            k = torch.zeros_like(q)
+            q[:, 0] = unit
+            # scores rise in steps of unit * unit / 64; from key to key, or with the last ones alike
+            k[:, 0] = unit + unit / 64 * (torch.arange(n, device="cuda") // 64).to(t)
+            v = torch.randint(-8, 9, (n, d), device="cuda").to(t)
+            for scale in (0.125, 1.0):
+                o = tw.tw_attention(q, k, v, None, 1, 1, scale, True)
+                s = (q[:, :1].double() @ k[:, :1].double().t()) * scale
+                s = s.masked_fill(torch.arange(n, device="cuda") > torch.arange(n, device="cuda")[:, None], float("-inf"))
+                want = torch.softmax(s, 1) @ v.double()
+                # the largest weights are alike, and off by half a step as all are; the others are 0
+                bound = torch.finfo(t).eps / 2 * (want.abs() + torch.softmax(s, 1) @ v.double().abs()) + 512 * U * 8 + 2.0 ** -25
+                assert ((o.double() - want).abs() / bound).max().item() <= 1.0
+                # the same beside a value that is not finite, which the rows before the last do not see
+                v2 = v.clone()
+                v2[n - 1] = float("inf")
+                o2 = tw.tw_attention(q, k, v2, None, 1, 1, scale, True)[:n - 1]
+                assert ((o2.double() - want[:n - 1]).abs() / bound[:n - 1]).max().item() <= 1.0
+        # sums of many large products, whose order shows: whatever the largest is, a result lies among the values
+        gen = torch.Generator(device="cuda").manual_seed(5)
+        q, k = ((torch.randn((n, d), generator=gen, device="cuda") * 8000).to(t) for _ in range(2))
+        v = 3.0 + torch.rand((n, d), generator=gen, device="cuda").to(t)
+        v[n - 1] = float("inf")
+        for causal in (True, False):
+            o = tw.tw_attention(q, k, v, torch.tensor([0, n - 1, n], dtype=torch.int32, device="cuda"), 1, 1, 1.0, causal)[:n - 1]
+            assert bool(((o >= 3.0) & (o <= 4.0)).all())
