@@ -225,7 +225,10 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
     for (int f = 0; f < FB; ++f)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[f][r] = 0.f;
-    // ref: what the exponents are taken from, at least the running maximum less kSlack; l: this lane's share of the sum of weights
+    // ref: what the exponents are taken from, between the running maximum less kSlack + kLift and that less kLift; l: this lane's share of the sum of weights.
+    // f16 holds nothing below 2^-24, which thousands of keys that one outweighs may lie below: its weights are taken 2^7 times as large, so that the
+    // largest lies between 2^7 and 2^15 and a small one is off by 2^-32 of it at most.
+    constexpr float kLift = DT == TW_F16 ? 7.f : 0.f;
     float ref = -__builtin_inff(), l = 0.f;
 
     // Where this lane's operands lie in a tile.  Scores: row (key) 32 b + l32, piece (2 ks + h) ^ fk; values: rows 16 st + 4 h + j / 4 (+ 8), piece
@@ -307,9 +310,9 @@ __global__ __launch_bounds__(256, 2) void tw_attention_kernel(const AttnParams p
             for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[b][r]);
         top = max_halves(top) * scale2;
         // The exponents' reference moves only when some row's maximum has grown by more than kSlack powers of two: the weights stay below
-        // 2^kSlack, which 16 bits hold as precisely, and most tiles scale nothing.
-        if (__any(top - ref > kSlack)) {                     // (the difference: a step of the sum may be larger than the slack)
-            const float next_ref = __builtin_fmaxf(ref, top);
+        // 2^(kSlack + kLift), which 16 bits hold as precisely, and most tiles scale nothing.
+        if (__any(top - ref > kSlack + kLift)) {             // (the difference: a step of the sum may be larger than the slack)
+            const float next_ref = __builtin_fmaxf(ref, top - kLift);
             const float from = ref == -__builtin_inff() ? next_ref : ref;     // (nothing summed yet; -inf twice: no key seen)
             const float fade = __builtin_amdgcn_exp2f(ref == next_ref ? 0.f : from - next_ref);
             ref = next_ref;

@@ -338,3 +338,31 @@ def test_scores_beyond_what_a_step_of_fp32_resolves():
         for causal in (True, False):
             o = tw.tw_attention(q, k, v, torch.tensor([0, n - 1, n], dtype=torch.int32, device="cuda"), 1, 1, 1.0, causal)[:n - 1]
             assert bool(((o >= 3.0) & (o <= 4.0)).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_many_keys_of_little_weight(dtype):
+    """One key outweighs each of the others by 2^25, and has nothing to give: the result is what the others give together.
+
+    f16: the largest weight of a row is 2^7 at least, so that one below the smallest normal number is off by 2^-25 of 2^7 at most, 2^-32 of the
+    largest; a normal one by half a step, and a result by half a step (and fp32 as above: (d + 8 + 2 (n + 64)) units and more, below 2^-6 of
+    eps / 2 here for bf16, and below 2^-4 of the result for f16)."""
+    n, d = 32768, 16
+    t = TYPES[dtype]
+    q = torch.zeros((n, d), dtype=t, device="cuda")
+    k, v = torch.zeros_like(q), torch.ones_like(q)
+    q[:, 0], k[:, 0] = 1.0, -17.5
+    for where in (0, 20000, n - 1):
+        k[:, 0] = -17.5
+        k[where], v[:] = 0.0, 1.0
+        v[where] = 0.0
+        for causal in (False, True):
+            o = tw.tw_attention(q, k, v, None, 1, 1, 1.0, causal).double()
+            seen = torch.arange(1, n + 1, device="cuda", dtype=torch.float64) if causal else torch.full((n,), float(n), device="cuda", dtype=torch.float64)
+            w = torch.exp(torch.tensor(-17.5, dtype=torch.float64)).item()
+            sink = (torch.arange(n, device="cuda") >= where) if causal else torch.ones(n, dtype=torch.bool, device="cuda")
+            want = torch.where(sink, (seen - 1) * w / (1 + (seen - 1) * w), 1.0)
+            eps2 = torch.finfo(t).eps / 2
+            fp32 = (d + 8 + 2 * (seen + 64)) * U * 2 * want
+            bound = 2 * eps2 * want + fp32 + (seen * 2.0 ** -32 + 2.0 ** -25 if t == torch.float16 else 0.0)
+            assert bool(((o - want[:, None]).abs() <= bound[:, None]).all())
