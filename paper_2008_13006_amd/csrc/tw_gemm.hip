@@ -734,25 +734,29 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
         };
 
         // clear both planes once: the passes all write the same columns.  With a fused epilogue a pruned
-        // column holds act(bias) in every row instead of zero.
+        // column holds act(bias) in every row instead of zero.  (kAdd: every pass puts the rows that are added over both planes and then
+        // writes all columns of the span, the pruned ones too; there is nothing to clear.)
         tw_compiler_fence();
-        if (!fused || FUSED == kAdd || d.span_w == d.w) {
+        if constexpr (FUSED != kAdd) {
+            if (!fused || d.span_w == d.w) {
 #pragma unroll
-            for (int pl = 0; pl < 2; ++pl)
+                for (int pl = 0; pl < 2; ++pl)
 #pragma unroll
-                for (int i = 0; i < kCols * 8 / 1024; ++i)
-                    *(tw_u32x4*)(stage + pl * kPlane + i * 1024 + lane * 16) = tw_u32x4{0u, 0u, 0u, 0u};
-        } else {
+                    for (int i = 0; i < kCols * 8 / 1024; ++i)
+                        *(tw_u32x4*)(stage + pl * kPlane + i * 1024 + lane * 16) = tw_u32x4{0u, 0u, 0u, 0u};
+            } else {
 #pragma unroll
-            for (int l = 0; l < WL; ++l) {
-                const int c = win0 + l * kLineCols + lane;
-                float b = eb.fill[l];
-                if (win0 != W0) b = (p.bias != nullptr && c >= S && c < E) ? tw_to_f32<DT>(p.bias[c]) : 0.f;   // later windows: read here
-                const unsigned hv = (c >= S && c < E) ? (unsigned)tw_cvt<DT>(tw_activate(b, p.act)) : 0u;
-                const tw_u32x2 v{hv | (hv << 16), hv | (hv << 16)};
-                *(tw_u32x2*)(stage + (l * kLineCols + lane) * 8) = v;
-                *(tw_u32x2*)(stage + kPlane + (l * kLineCols + lane) * 8) = v;
+                for (int l = 0; l < WL; ++l) {
+                    const int c = win0 + l * kLineCols + lane;
+                    float b = eb.fill[l];
+                    if (win0 != W0) b = (p.bias != nullptr && c >= S && c < E) ? tw_to_f32<DT>(p.bias[c]) : 0.f;   // later windows: read here
+                    const unsigned hv = (c >= S && c < E) ? (unsigned)tw_cvt<DT>(tw_activate(b, p.act)) : 0u;
+                    const tw_u32x2 v{hv | (hv << 16), hv | (hv << 16)};
+                    *(tw_u32x2*)(stage + (l * kLineCols + lane) * 8) = v;
+                    *(tw_u32x2*)(stage + kPlane + (l * kLineCols + lane) * 8) = v;
+                }
             }
+            tw_compiler_fence();
         }
         tw_compiler_fence();
 #pragma unroll
