@@ -436,8 +436,17 @@ constexpr unsigned kStageBytes = 2 * kPlaneBytes;   // per wave
 // takes several, which costs the wave its staging again.)
 constexpr int kNarrowLines = 2;
 template <int WL> constexpr int plane_bytes() { return WL * kLineCols * 8 + 32 * 8 + 32; }
-static_assert(plane_bytes<kWinLines>() == kPlaneBytes && plane_bytes<kNarrowLines>() % 16 == 0 && (plane_bytes<kNarrowLines>() / 4) % 16 == 8, "plane skew");
+static_assert(plane_bytes<kWinLines>() == kPlaneBytes && plane_bytes<kNarrowLines>() % 16 == 0 && (plane_bytes<kNarrowLines>() / 4) % 16 == 8 &&
+              plane_bytes<3>() % 16 == 0 && (plane_bytes<3>() / 4) % 16 == 8, "plane skew");
 constexpr unsigned kNarrowStageBytes = 2 * plane_bytes<kNarrowLines>();
+// Lines of the windows of a kernel that has room for `most`.  Where rows are added to the widest tiles (128 accumulators a lane), windows of
+// four lines leave 4 to 9 registers in scratch memory, three none (a span of 128 columns fits three as a rule); with the code for TEW
+// blobs two leave the least.
+template <int FUSED, int NCB, bool EW>
+constexpr int window_lines(int most) {
+    const int fit = EW ? kNarrowLines : 3;
+    return FUSED == kAdd && NCB == 4 && most > fit ? fit : most;
+}
 static_assert(kPlaneBytes % 16 == 0 && (kPlaneBytes / 4) % 16 == 8, "plane skew");
 
 __device__ __forceinline__ void tw_compiler_fence() { asm volatile("" ::: "memory"); }
@@ -680,7 +689,6 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
                 *(unsigned short*)(stage + ((lane >> 2) & 1) * kPlane + rel * 8u + (lane & 3) * 2) = tw_cvt<DT>(x);
         };
         auto write_pass = [&](int P) {
-            const int ms = P >> 2, q = P & 3;
             unsigned short add[NCB][4], zadd[kFillAhead];
             if constexpr (FUSED == kAdd) {
 #pragma unroll
@@ -702,16 +710,28 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
                 }
                 tw_compiler_fence();
             }
-            auto value = [&](int cb, int i) {
-                if constexpr (FUSED == kAdd) return acc[ms][cb][4 * q + i] + tw_to_f32<DT>(add[cb][i]);
-                else return acc[ms][cb][4 * q + i];
-            };
+            // (the accumulators of a pass have to be named by constants)
 #pragma unroll
-            for (int cb = 0; cb < NCB; ++cb) {
-                tw_u32x2 v;
-                v.x = (unsigned)tw_cvt<DT>(value(cb, 0)) | ((unsigned)tw_cvt<DT>(value(cb, 1)) << 16);
-                v.y = (unsigned)tw_cvt<DT>(value(cb, 2)) | ((unsigned)tw_cvt<DT>(value(cb, 3)) << 16);
-                *(tw_u32x2*)wpos[cb] = v;
+            for (int k = 0; k < NP; ++k) {
+                if (k != P) continue;                        // wave-uniform
+                const int ms = k >> 2, q = k & 3;
+                auto value = [&](int cb, int i) {
+                    if constexpr (FUSED == kAdd) return acc[ms][cb][4 * q + i] + tw_to_f32<DT>(add[cb][i]);
+                    else return acc[ms][cb][4 * q + i];
+                };
+#pragma unroll
+                for (int cb = 0; cb < NCB; ++cb) {
+                    tw_u32x2 v;
+                    v.x = (unsigned)tw_cvt<DT>(value(cb, 0)) | ((unsigned)tw_cvt<DT>(value(cb, 1)) << 16);
+                    v.y = (unsigned)tw_cvt<DT>(value(cb, 2)) | ((unsigned)tw_cvt<DT>(value(cb, 3)) << 16);
+                    *(tw_u32x2*)wpos[cb] = v;
+                }
+                if (nx > 0) {                                // wave-uniform
+#pragma unroll
+                    for (int g = 0; g < TW_XC_INLINE / 8; ++g)
+                        if (xpos[g] != nullptr)
+                            *(unsigned short*)xpos[g] = (unsigned short)(xq[g][k >> 1] >> (16 * (k & 1)));
+                }
             }
             if constexpr (FUSED == kAdd) {
 #pragma unroll
@@ -724,12 +744,6 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
                     const int r = 8 * P + (lane & 7);
                     if (col >= 0) put_pruned(col, base + tw_to_f32<DT>(p.res[(long)(row0 + (r < rlast ? r : rlast)) * p.ldr + col]));
                 }
-            }
-            if (nx > 0) {                                    // wave-uniform
-#pragma unroll
-                for (int g = 0; g < TW_XC_INLINE / 8; ++g)
-                    if (xpos[g] != nullptr)
-                        *(unsigned short*)xpos[g] = (unsigned short)(xq[g][P >> 1] >> (16 * (P & 1)));
             }
         };
 
@@ -759,16 +773,7 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
             tw_compiler_fence();
         }
         tw_compiler_fence();
-#pragma unroll
-        for (int P = 0; P < NP; ++P)
-            if (P == pass0) {
-                request_add(P, win0);
-                write_pass(P);
-            }
-        tw_compiler_fence();
-#pragma unroll
-        for (int P = 0; P < NP; ++P) {
-            if (P < pass0 || P >= pass1) continue;               // wave-uniform
+        auto store_pass = [&](int P) __attribute__((always_inline)) {
             tw_i16x4 lo[WL], hi[WL];
 #pragma unroll
             for (int l = 0; l < WL; ++l) {
@@ -798,6 +803,24 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
             // pipeline holds up the loads of the waves that are multiplying (no load of this wave is pending here).
             // (kAdd: the waits for what is added see to that; this one would wait for what has been asked for ahead.)
             if constexpr (FUSED != kAdd) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+        };
+        if constexpr (FUSED == kAdd) {
+            // (a loop: unrolled, the branches of eight passes around the accumulators end in scratch memory)
+            request_add(pass0, win0);
+            write_pass(pass0);
+            tw_compiler_fence();
+#pragma unroll 1
+            for (int P = pass0; P < pass1; ++P) store_pass(P);
+        } else {
+#pragma unroll
+            for (int P = 0; P < NP; ++P)
+                if (P == pass0) write_pass(P);
+            tw_compiler_fence();
+#pragma unroll
+            for (int P = 0; P < NP; ++P) {
+                if (P < pass0 || P >= pass1) continue;           // wave-uniform
+                store_pass(P);
+            }
         }
         tw_compiler_fence();
     }
@@ -1532,7 +1555,7 @@ __global__ __launch_bounds__(kThreads) void tw_gemm_kernel(const TwGemmParams p)
                                            p.blob + p.off_bvals + (long)d.first_step * NCB * 1024, 0, d.nsteps, lane);
                 if (has_ew) add_ew_residual<DT, MS, NCB>(p, d.tile, 0, acc, smem, at_pitch_of<MS>(), lane);
                 if constexpr (TRANS) store_tile_t<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, 0, NCB, xbuf);
-                else store_tile<DT, MS, NCB, FUSED, false, WL>(p, d, acc, stage, dpos, row0, lane, xbuf, xcols);
+                else store_tile<DT, MS, NCB, FUSED, false, window_lines<FUSED, NCB, EW>(WL)>(p, d, acc, stage, dpos, row0, lane, xbuf, xcols);
             }
             __syncthreads();  // everyone is done with the LDS copy of A and with misc[]
         } else if constexpr (MODE == 2) {
@@ -1718,7 +1741,7 @@ __global__ __launch_bounds__(kThreads) void tw_gemm_kernel(const TwGemmParams p)
                 if (active) {
                     if (xbuf != nullptr) xc_finish<DT, MS, FUSED, TRANS>(p, d, stage, xbuf, row0, lane);
                     if constexpr (TRANS) store_tile_t<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, 0, NCB, xbuf);
-                    else store_tile<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, xbuf, xcols);
+                    else store_tile<DT, MS, NCB, FUSED, false, window_lines<FUSED, NCB, EW>(kWinLines)>(p, d, acc, stage, dpos, row0, lane, xbuf, xcols);
                 }
             }
         } else {
@@ -1862,7 +1885,7 @@ __global__ __launch_bounds__(kThreads) void tw_gemm_kernel(const TwGemmParams p)
                 } else {
                     if (xbuf != nullptr) xc_finish<DT, MS, FUSED, TRANS>(p, d, stage, xbuf, row0, lane);
                     if constexpr (TRANS) store_tile_t<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, 0, NCB, xbuf);
-                    else store_tile<DT, MS, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane, xbuf, xcols);
+                    else store_tile<DT, MS, NCB, FUSED, false, window_lines<FUSED, NCB, EW>(kWinLines)>(p, d, acc, stage, dpos, row0, lane, xbuf, xcols);
                 }
             }
         }
@@ -2624,7 +2647,9 @@ const void* pick_stream(int ncb) {
     switch (ncb) {
         case 1: return (const void*)tw_stream_kernel<DT, 1, FUSED>;
         case 2: return (const void*)tw_stream_kernel<DT, 2, FUSED>;
-        case 4: return (const void*)tw_stream_kernel<DT, 4, FUSED>;
+        case 4:
+            if constexpr (FUSED != kAdd) return (const void*)tw_stream_kernel<DT, 4, FUSED>;
+            return nullptr;                       // (plan_stream)
         default: return nullptr;
     }
 }
@@ -3273,8 +3298,9 @@ void plan_rows(const TwHeader* h, int M, long lda, int n_cu, Plan& pl, bool gelu
 // and pitches whose rows lie too far apart for 32-bit offsets.  (5400 random calls: 1.25 times as fast on average, see there.)
 constexpr long kFarPitch = 1 << 23;
 unsigned stream_lds_bytes() { return 2 * at_bytes(2, kStreamChunk) + kStreamTiles * kStageBytes + kWindows * kWindowBytes; }
-void plan_stream(const TwHeader* h, long lda, Plan& pl) {
+void plan_stream(const TwHeader* h, long lda, Plan& pl, bool add) {
     pl.stream_items = 0;
+    if (add && h->ncb == 4) return;
     if (pl.mode != 2 || pl.n_parts > 1 || h->k_chunk != kStreamChunk || h->ew_nnz > 0 || lda >= kFarPitch) return;
     pl.stream_items = pl.n_items;
 }
@@ -3529,7 +3555,7 @@ int run_gemm(const void* blob_host, const void* blob_dev, const void* A, int M, 
     Plan pl;
     int rc = make_plan(h, M, n_cu, pl, false, ws_bytes, act == TW_ACT_GELU);
     if (rc) return rc;
-    plan_stream(h, lda, pl);
+    plan_stream(h, lda, pl, R != nullptr);
     const bool split = pl.n_parts > 1;
     const int epilogue = R != nullptr ? kAdd : bias != nullptr || act != TW_ACT_NONE ? kFused : kPlain;
     const int epi = split ? kPlain : epilogue;        // split K: the epilogue is the second kernel's

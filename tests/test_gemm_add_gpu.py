@@ -297,3 +297,42 @@ def test_streams_and_graphs(tw):
         torch.cuda.synchronize()
         got = C.clone(), Ct.clone()
         assert torch.equal(got[0], tw.tw_gemm_bias_act_add(wt, A, R)) and torch.equal(got[1], tw.tw_gemm_t_bias_act_add(wt, At, Rt))
+
+
+MEMORY_CHILD = """
+import sys
+sys.path.insert(0, {root!r})
+import torch
+from paper_2008_13006_amd import binding as tw, workloads as W
+modes = set()
+for dtype, t in (("f16", torch.float16), ("bf16", torch.bfloat16)):
+    for M, K, N in ((16384, 768, 768), (16384, 2304, 768), (8192, 4096, 1024)):
+        w = W.generate(W.small_spec("memory", M=1, K=K, N=N, G=128, dtype=dtype, col_prune=0.05, keep=("upow", 0.1, 0.4), seed_offset=9500))
+        weight = tw.TwWeight(tw.tw_pack(w.B, w.mask, 128, dtype))
+        modes.add(tw.tw_gemm_plan(weight.blob, M)["mode"])
+        a, r, c = (torch.zeros(s, dtype=t, device="cuda") for s in ((M, K), (M, N), (M, N)))
+        # (what the call below needs of the library's code is loaded: that of the products without R, and of those with it by the other boundary's)
+        tw.tw_gemm_bias_act(weight, a, None, "relu", c)
+        at, ct = torch.zeros((K, 64), dtype=t, device="cuda"), torch.zeros((N, 64), dtype=t, device="cuda")
+        tw.tw_gemm_t_bias_act_add(weight, at, ct, None, "relu", torch.empty_like(ct))
+        torch.cuda.synchronize()
+        before = torch.cuda.mem_get_info()[0]
+        tw.tw_gemm_bias_act_add(weight, a, r, None, "relu", c)
+        torch.cuda.synchronize()
+        print("taken", (before - torch.cuda.mem_get_info()[0]) >> 20, "MB", dtype, M, K, N, flush=True)
+print("modes", sorted(modes), flush=True)
+"""
+
+
+def test_first_calls_take_no_device_memory():
+    """The library allocates no device memory, and neither does the runtime for its kernels: one whose registers spill has memory set aside for every
+    lane of the card at its first call.  A process of its own, in which no other kernel has been run."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    child = subprocess.run([sys.executable, "-c", MEMORY_CHILD.format(root=root)], capture_output=True, text=True, timeout=100)
+    assert child.returncode == 0, child.stderr[-2000:]
+    taken = [line.split() for line in child.stdout.splitlines() if line.startswith("taken")]
+    assert len(taken) == 6 and "modes [0, 1, 2]" in child.stdout, child.stdout
+    assert all(int(words[1]) == 0 for words in taken), child.stdout
