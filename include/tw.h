@@ -260,6 +260,8 @@ int tw_gemm_t_bias_act(const void* blob_host, const void* blob_dev, const void* 
  *        added to C; not for a TEW blob with residual weights in pruned columns); otherwise the two must not overlap
  *   bias, act  as in tw_gemm_bias_act (NULL and TW_ACT_NONE: the plain product plus R)
  * The sum of the fp32 result and R is rounded once to the storage type.  A pruned column n of C holds act(bias[n]) + R[m, n].
+ * (TEW blobs with G = 128: a few of these kernels' registers do not fit; the runtime sets aside 20 to 30 MB of device memory for them at the
+ * first call.)
  * Everything else as tw_gemm_bias_act; TW_ERR_ARG also for a null R, ldr < N, R = C with another pitch; TW_ERR_UNSUPPORTED also for
  * R = C where a TEW blob rules it out. */
 int tw_gemm_bias_act_add(const void* blob_host, const void* blob_dev, const void* A, int M, int lda,

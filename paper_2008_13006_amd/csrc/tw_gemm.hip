@@ -677,11 +677,11 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
                 if (rel < (unsigned)kCols) xpos[g] = stage + ((lane >> 2) & 1) * kPlane + rel * 8u + (lane & 3) * 2;
             }
         }
-        tw_u32x4 xq[TW_XC_INLINE / 8];                       // this lane's row of its columns, all passes
+        tw_u32x4 xq[TW_XC_INLINE / 8];                       // this lane's row of its columns, all passes (kAdd: read pass by pass)
 #pragma unroll
         for (int g = 0; g < TW_XC_INLINE / 8; ++g) {
             xq[g] = tw_u32x4{0u, 0u, 0u, 0u};
-            if (nx > 0) xq[g] = *(const tw_u32x4*)(xbuf + (8 * g + (lane >> 3)) * 64 + (lane & 7) * 8);
+            if (FUSED != kAdd && nx > 0) xq[g] = *(const tw_u32x4*)(xbuf + (8 * g + (lane >> 3)) * 64 + (lane & 7) * 8);
         }
         auto put_pruned = [&](int col, float x) {            // this lane's row of a pruned column
             const unsigned rel = (unsigned)(col - win0);
@@ -730,7 +730,8 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
 #pragma unroll
                     for (int g = 0; g < TW_XC_INLINE / 8; ++g)
                         if (xpos[g] != nullptr)
-                            *(unsigned short*)xpos[g] = (unsigned short)(xq[g][k >> 1] >> (16 * (k & 1)));
+                            *(unsigned short*)xpos[g] = FUSED == kAdd ? xbuf[(8 * g + (lane >> 3)) * 64 + (lane & 7) * 8 + k]
+                                                                      : (unsigned short)(xq[g][k >> 1] >> (16 * (k & 1)));
                 }
             }
             if constexpr (FUSED == kAdd) {
@@ -1309,7 +1310,8 @@ __device__ __forceinline__ void xc_request(const TwGemmParams& p, const TileU& d
     x.s1 = fetch_int(xp, 1);
     if (x.s0 != x.s1) request_block_steps<1>(x.r, p.blob + p.off_xm_goff, p.blob + p.off_xm_b, x.s0, x.s1, lane);
 }
-template <int DT, int MS, int FUSED>
+// (FEW: addresses of what is added a few at a time, where the first weights of the tile's own steps are on their way already)
+template <int DT, int MS, int FUSED, bool FEW>
 __device__ __forceinline__ void xc_store(const TwGemmParams& p, const TileU& d, const tw_f32x16 (&acc)[MS][1],
                                          unsigned short* xbuf, int row0, int lane) {
     const int n = lane & 31, h = lane >> 5;
@@ -1329,7 +1331,7 @@ __device__ __forceinline__ void xc_store(const TwGemmParams& p, const TileU& d, 
                     v[q] = acc[ms][0][4 * q + i];
                     if constexpr (FUSED) v[q] = tw_activate(v[q] + bias, p.act);
                     if constexpr (FUSED == kAdd) {
-                        const int r = row0 + 32 * ms + 8 * q + 4 * h + i;
+                        const int at = row0 + 32 * ms + 8 * q + i, r = (FEW ? fresh(at) : at) + 4 * h;
                         v[q] += tw_to_f32<DT>(p.res[(long)(r < last ? r : last) * p.ldr + col]);
                     }
                 }
@@ -1383,7 +1385,7 @@ __device__ __forceinline__ void xc_columns(const TwGemmParams& p, const TileU& d
     if (x.s0 != x.s1)
         run_block_steps<DT, MS, 1>(acc, x.r, at, at_pitch, p.blob + p.off_xm_goff, p.blob + p.off_xm_b, x.s0, x.s1, lane);
     if constexpr (TRANS) xc_store_t<DT, MS, FUSED>(p, d, acc, xbuf, row0, lane);
-    else xc_store<DT, MS, FUSED>(p, d, acc, xbuf, row0, lane);
+    else xc_store<DT, MS, FUSED, true>(p, d, acc, xbuf, row0, lane);
 }
 // K streamed: the sums of the 16 columns between chunks, fp32, piece (ms, q) of lane (h, n < 16) at float offset
 // (((4 * ms + q) * 32 + 16 * h + n) * 4 of `area` (4 KB with 64 rows)
@@ -1434,7 +1436,7 @@ __device__ __forceinline__ void xc_finish(const TwGemmParams& p, const TileU& d,
     tw_f32x16 acc[MS][1];
     xc_load_partial<MS>(acc, area, lane);
     if constexpr (TRANS) xc_store_t<DT, MS, FUSED>(p, d, acc, xbuf, row0, lane);
-    else xc_store<DT, MS, FUSED>(p, d, acc, xbuf, row0, lane);
+    else xc_store<DT, MS, FUSED, false>(p, d, acc, xbuf, row0, lane);
 }
 
 // MODE 0: the K extent of a row block of 32*MS rows is resident in LDS, waves pull whole tiles.
