@@ -710,28 +710,40 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
                 }
                 tw_compiler_fence();
             }
-            // (the accumulators of a pass have to be named by constants)
+            if constexpr (FUSED == kAdd) {
+                // (the accumulators of a pass have to be named by constants)
 #pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                if (k != P) continue;                        // wave-uniform
-                const int ms = k >> 2, q = k & 3;
-                auto value = [&](int cb, int i) {
-                    if constexpr (FUSED == kAdd) return acc[ms][cb][4 * q + i] + tw_to_f32<DT>(add[cb][i]);
-                    else return acc[ms][cb][4 * q + i];
-                };
+                for (int k = 0; k < NP; ++k) {
+                    if (k != P) continue;                    // wave-uniform
+                    const int ms = k >> 2, q = k & 3;
+                    auto value = [&](int cb, int i) { return acc[ms][cb][4 * q + i] + tw_to_f32<DT>(add[cb][i]); };
+#pragma unroll
+                    for (int cb = 0; cb < NCB; ++cb) {
+                        tw_u32x2 v;
+                        v.x = (unsigned)tw_cvt<DT>(value(cb, 0)) | ((unsigned)tw_cvt<DT>(value(cb, 1)) << 16);
+                        v.y = (unsigned)tw_cvt<DT>(value(cb, 2)) | ((unsigned)tw_cvt<DT>(value(cb, 3)) << 16);
+                        *(tw_u32x2*)wpos[cb] = v;
+                    }
+                    if (nx > 0) {                            // wave-uniform
+#pragma unroll
+                        for (int g = 0; g < TW_XC_INLINE / 8; ++g)
+                            if (xpos[g] != nullptr) *(unsigned short*)xpos[g] = xbuf[(8 * g + (lane >> 3)) * 64 + (lane & 7) * 8 + k];
+                    }
+                }
+            } else {
+                const int ms = P >> 2, q = P & 3;
 #pragma unroll
                 for (int cb = 0; cb < NCB; ++cb) {
                     tw_u32x2 v;
-                    v.x = (unsigned)tw_cvt<DT>(value(cb, 0)) | ((unsigned)tw_cvt<DT>(value(cb, 1)) << 16);
-                    v.y = (unsigned)tw_cvt<DT>(value(cb, 2)) | ((unsigned)tw_cvt<DT>(value(cb, 3)) << 16);
+                    v.x = (unsigned)tw_cvt<DT>(acc[ms][cb][4 * q + 0]) | ((unsigned)tw_cvt<DT>(acc[ms][cb][4 * q + 1]) << 16);
+                    v.y = (unsigned)tw_cvt<DT>(acc[ms][cb][4 * q + 2]) | ((unsigned)tw_cvt<DT>(acc[ms][cb][4 * q + 3]) << 16);
                     *(tw_u32x2*)wpos[cb] = v;
                 }
                 if (nx > 0) {                                // wave-uniform
 #pragma unroll
                     for (int g = 0; g < TW_XC_INLINE / 8; ++g)
                         if (xpos[g] != nullptr)
-                            *(unsigned short*)xpos[g] = FUSED == kAdd ? xbuf[(8 * g + (lane >> 3)) * 64 + (lane & 7) * 8 + k]
-                                                                      : (unsigned short)(xq[g][k >> 1] >> (16 * (k & 1)));
+                            *(unsigned short*)xpos[g] = (unsigned short)(xq[g][P >> 1] >> (16 * (P & 1)));
                 }
             }
             if constexpr (FUSED == kAdd) {
