@@ -549,7 +549,9 @@ __device__ __forceinline__ void apply_bias_act4(tw_f32x4 (&v)[NV], const float (
 // FUSED: the kernel variant with the fused epilogue (a bias and / or an activation); the plain variant
 // carries none of its code.  PART: a wave that stores a part of the tile; bias and activation have been applied (pruned
 // columns inside the span still take theirs here).
-template <int DT, int MS, int NCB, int FUSED, bool PART = false, int WL = kWinLines>
+// LOOP (kAdd): the passes are a loop.  Unrolled, the branches of eight passes around 128 accumulators end in scratch memory, up to 106 registers and 1.3 times
+// the time on 16384 x 768 -> 768; narrower tiles fit, and the loop costs them 4 to 6 %, waves with a part of a tile 3 %.
+template <int DT, int MS, int NCB, int FUSED, bool PART = false, int WL = kWinLines, bool LOOP = NCB == 4 && !PART>
 __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d, tw_f32x16 (&acc)[MS][NCB],
                                            unsigned char* stage, const unsigned (&dpos)[NCB], int row0, int lane_in,
                                            unsigned short* xbuf = nullptr,
@@ -817,8 +819,7 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
             // (kAdd: the waits for what is added see to that; this one would wait for what has been asked for ahead.)
             if constexpr (FUSED != kAdd) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
         };
-        if constexpr (FUSED == kAdd) {
-            // (a loop: unrolled, the branches of eight passes around the accumulators end in scratch memory)
+        if constexpr (FUSED == kAdd && LOOP) {
             request_add(pass0, win0);
             write_pass(pass0);
             tw_compiler_fence();
@@ -827,7 +828,10 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
         } else {
 #pragma unroll
             for (int P = 0; P < NP; ++P)
-                if (P == pass0) write_pass(P);
+                if (P == pass0) {
+                    if constexpr (FUSED == kAdd) request_add(P, win0);
+                    write_pass(P);
+                }
             tw_compiler_fence();
 #pragma unroll
             for (int P = 0; P < NP; ++P) {
@@ -2486,7 +2490,7 @@ __global__ __launch_bounds__(kThreads) void tw_stream_kernel(const TwGemmParams 
             s2 = fetch_int(sp, c + 3 < p.n_chunks ? c + 3 : p.n_chunks);
             buf = buf == 0 ? p.abuf_bytes : 0u;
         }
-        if (active) store_tile<DT, 2, NCB, FUSED>(p, d, acc, stage, dpos, row0, lane);
+        if (active) store_tile<DT, 2, NCB, FUSED, false, kWinLines, NCB >= 2>(p, d, acc, stage, dpos, row0, lane);
     }
 }
 
@@ -3314,6 +3318,8 @@ constexpr long kFarPitch = 1 << 23;
 unsigned stream_lds_bytes() { return 2 * at_bytes(2, kStreamChunk) + kStreamTiles * kStageBytes + kWindows * kWindowBytes; }
 void plan_stream(const TwHeader* h, long lda, Plan& pl, bool add) {
     pl.stream_items = 0;
+    // (with R and 128 accumulators a lane its multiplying waves leave 70 to 150 registers in scratch memory, the plan's kernel none: 8192 x 4096 -> 1024
+    // 57 us (bf16 97) -> 46; narrower tiles fit)
     if (add && h->ncb == 4) return;
     if (pl.mode != 2 || pl.n_parts > 1 || h->k_chunk != kStreamChunk || h->ew_nnz > 0 || lda >= kFarPitch) return;
     pl.stream_items = pl.n_items;
