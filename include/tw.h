@@ -161,8 +161,8 @@ typedef struct tw_plan_t {
     int32_t n_items;         /* work items = n_row_blocks * n_sets * k_parts */
     int32_t grid;            /* workgroups launched: min(n_items, n_cu), each pulls items until none is left */
     uint32_t lds_bytes;      /* on-chip memory per workgroup (tw_gemm with mode 2: of the transposed kernel's layout without its row
-                                lists; its own kernel, which runs but where a matrix is added with G = 128, takes 155 KB whatever the weight.  tw_gemm with k_parts > 1: of the first kernel,
-                                for lda < 2^23; TEW blobs and rows further apart take another kernel with 141 KB) */
+                                lists; its own kernel, which runs but where a matrix is added with G = 128, takes 155 KB whatever
+                                the weight.  tw_gemm with k_parts > 1: of the first kernel, for lda < 2^23; TEW blobs and rows further apart take another kernel with 141 KB) */
     int32_t row_lists;       /* tw_gemm_t, mode 2: the loading waves read only the K rows that the tiles keep */
     int32_t k_parts;         /* streamed K, few row blocks: the K chunks are split into this many parts, each a work item
                                 of its own (n_items = n_row_blocks * n_sets * k_parts) whose fp32 results go to the
@@ -355,12 +355,15 @@ int tw_layernorm_grad(const void* dY, int lddy, const void* X, int ldx, int M, i
  *   heads      a multiple of kv_heads
  *   head_dim   a multiple of 8, at most 128
  *   scale      >= 0 and finite (1 / sqrt(head_dim) as a rule)
- * Scores, softmax statistics and sums are fp32; the weights p are rounded to dt for the product with V, O is rounded once.  A token that a row
+ * Scores, softmax statistics and sums are fp32; the weights p are rounded to dt for the product with V (f16: those below 2^-21 of a row's largest
+ * by 2^-32 of it at most), O is rounded once.  A token that a row
  * does not see leaves it untouched, whatever its values; non-finite scores or values that it sees give what the formula gives in
- * fp32 (a weight that underflows to zero beside an infinite value: NaN or that infinity).
+ * fp32 (a weight that underflows to zero beside an infinite value: NaN or that infinity).  Values of V that are not finite cost time: 32 rows that
+ * see some of such a token's neighbours, but not all of them the token, are summed key by key, 6 us a key (one such token amid a prompt
+ * of 8192: 24 ms instead of 0.3; all of V: 50).
  * M >= 0 (M = 0 enqueues nothing).  One kernel, no workspace; it can be recorded into a HIP graph (the lengths are read when it runs).
- * Errors: TW_ERR_ARG (null pointer, negative M or n_seqs, heads not a multiple of kv_heads, pitch too small, O = Q with another pitch, scale, unknown dt, no
- * seq_start and n_seqs > 1), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED (head_dim; ldk or ldv of 2^24 and more; heads * ceil(M / 128) of 2^24
+ * Errors: TW_ERR_ARG (null pointer, negative M or n_seqs, heads not a multiple of kv_heads, pitch too small, O = Q with another pitch, scale,
+ * unknown dt, no seq_start and n_seqs > 1), TW_ERR_ALIGN, TW_ERR_UNSUPPORTED (head_dim; ldk or ldv of 2^24 and more; heads * ceil(M / 128) of 2^24
  * and more; a scale above 2.3e38), TW_ERR_HIP. */
 int tw_attention(const void* Q, int ldq, const void* K, int ldk, const void* V, int ldv, void* O, int ldo, int M,
                  const int* seq_start, int n_seqs, int heads, int kv_heads, int head_dim, float scale, int causal, tw_dtype dt,

@@ -549,8 +549,9 @@ __device__ __forceinline__ void apply_bias_act4(tw_f32x4 (&v)[NV], const float (
 // FUSED: the kernel variant with the fused epilogue (a bias and / or an activation); the plain variant
 // carries none of its code.  PART: a wave that stores a part of the tile; bias and activation have been applied (pruned
 // columns inside the span still take theirs here).
-// LOOP (kAdd): the passes are a loop.  Unrolled, the branches of eight passes around 128 accumulators end in scratch memory, up to 106 registers and 1.3 times
-// the time on 16384 x 768 -> 768; narrower tiles fit, and the loop costs them 4 to 6 %, waves with a part of a tile 3 %.
+// LOOP (kAdd): the passes are a loop.  Unrolled, the branches of eight passes around 128 accumulators leave 55 to 617 registers in scratch
+// memory, for which the runtime sets aside up to 800 MB of the card, and take 35.9 us on 16384 x 768 -> 768 (27.5 so).  Narrower tiles fit, and the
+// loop costs them 4 to 6 %, waves with a part of a tile 3 %.
 template <int DT, int MS, int NCB, int FUSED, bool PART = false, int WL = kWinLines, bool LOOP = NCB == 4 && !PART>
 __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d, tw_f32x16 (&acc)[MS][NCB],
                                            unsigned char* stage, const unsigned (&dpos)[NCB], int row0, int lane_in,
@@ -576,7 +577,7 @@ __device__ __forceinline__ void store_tile(const TwGemmParams& p, const TileU& d
     // kAdd: the eight rows that are added to a pass are read like the results are written (eight lanes a line of a row), a pass ahead, put into
     // the staging window row by row, and from there every lane takes the four values of each of its columns; then the window takes the
     // results.  (2-byte requests straight into that arrangement, 16 a pass, keep the compute unit's address unit busy:
-    // 8192 x 1024 -> 1024 23.4 us, this way 21.3; without an addition 18.0.  Rounding first and adding where whole rows are stored would
+    // 8192 x 1024 -> 1024 23.4 us, this way 22.3; without an addition 18.5.  Rounding first and adding where whole rows are stored would
     // cost less and round twice.)  Rows behind the block's last one repeat it; their results are not stored.
     // The pruned columns of the span hold act(bias) + what is added, which differs from row to row: every pass puts its eight rows of
     // them into the window too.  Lane l takes column l / 8 (and l / 8 + 8, ..) of the packer's list, row l % 8.
