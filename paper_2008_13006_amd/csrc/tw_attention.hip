@@ -17,7 +17,8 @@
 // come into two LDS buffers by direct loads, on their way while the tile before is multiplied.
 //
 // Bound: 2 d multiply-adds a key and row on the matrix unit, and one exponential a key and row beside them.  One prompt of 8192 tokens, 16
-// heads of 128, causal: 260 us, 1060 TFLOP/s of what the mask leaves (a large bf16 product reaches 1256 on the same card).  What did not pay
+// heads of 128, causal: 260 to 271 us from card to card, 1015 to 1060 TFLOP/s of what the mask leaves (a large bf16 product reaches 1256; f16
+// takes 7 % longer).  The matrix unit is busy for 54 % of the cycles, the vector unit issues for 52 %.  What did not pay
 // there: 32 keys at a time in three stages of one wave (353 us: what one wave issues to the matrix unit and to the vector unit does not
 // overlap; what two waves issue does, and two workgroups share a compute unit), eight waves whose halves take turns at the two units
 // (300 us, and twice the time on short prompts), higher wave priority around the products (no difference).
