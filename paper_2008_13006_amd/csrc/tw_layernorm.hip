@@ -139,6 +139,9 @@ __device__ __forceinline__ float deviation(float squares, float rest, float inv_
     return 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);
 }
 
+// The mean of both steps.  (The rest about an infinity is NaN, the mean that infinity.)
+__device__ __forceinline__ float both_steps(float mean, float rest) { return __builtin_fabsf(mean) < __builtin_inff() ? mean + rest : mean; }
+
 // Row-major, 16-byte pieces.  TPR threads of a workgroup of 256 share a row, thread t of them the pieces t, t + TPR, .. (PER of
 // them); TAIL: N is no multiple of 8, the last piece reaches into the row's pitch.
 // (16384 x 4096: 40 us, 6.7 TB/s with part of the data in the last-level cache; 512 x 768: 3.6 us, an empty kernel takes 2.4.)
@@ -196,7 +199,7 @@ __global__ __launch_bounds__(256) void tw_ln_kernel(const LnParams p) {
         r *= inv_n;
         const float rstd = deviation(q, r, inv_n, p.eps);
         if (mine && t == 0) {
-            if (p.mean) p.mean[m] = mean + r;
+            if (p.mean) p.mean[m] = both_steps(mean, r);
             if (p.rstd) p.rstd[m] = rstd;
         }
         us* out = p.y + m * p.ldy;
@@ -236,7 +239,7 @@ __global__ __launch_bounds__(256) void tw_ln_any_kernel(const LnParams p) {
         r *= inv_n;
         const float rstd = deviation(q, r, inv_n, p.eps);
         if (threadIdx.x == 0) {
-            if (p.mean) p.mean[m] = mean + r;
+            if (p.mean) p.mean[m] = both_steps(mean, r);
             if (p.rstd) p.rstd[m] = rstd;
         }
         us* out = p.y + m * p.ldy;
@@ -338,7 +341,7 @@ __global__ __launch_bounds__(64 * WAVES) void tw_ln_t_kernel(const LnParams p) {
     const float my_rest = waves_sum(red[2], lane) * inv_n, my_rstd = deviation(waves_sum(red[1], lane), my_rest, inv_n, p.eps);
     const long token = (long)blockIdx.x * (8 * PCS) + lane;
     if (wave == 0 && token < p.M) {
-        if (p.mean) p.mean[token] = my_mean + my_rest;
+        if (p.mean) p.mean[token] = both_steps(my_mean, my_rest);
         if (p.rstd) p.rstd[token] = my_rstd;
     }
     give(my_rstd, own[wave][0], lane);
@@ -424,7 +427,7 @@ __global__ __launch_bounds__(1024) void tw_ln_t_loop_kernel(const LnParams p) {
     const float my_rest = waves_sum(red[2], lane) * inv_n, my_rstd = deviation(waves_sum(red[1], lane), my_rest, inv_n, p.eps);
     const long token = (long)blockIdx.x * (8 * PCS) + lane;
     if (wave == 0 && token < p.M) {
-        if (p.mean) p.mean[token] = my_mean + my_rest;
+        if (p.mean) p.mean[token] = both_steps(my_mean, my_rest);
         if (p.rstd) p.rstd[token] = my_rstd;
     }
     give(my_rstd, own[wave][0], lane);
@@ -476,7 +479,7 @@ __global__ __launch_bounds__(1024) void tw_ln_t_any_kernel(const LnParams p) {
     const float rstd = deviation(sum(1), rest, inv_n, p.eps);
     if (m >= p.M) return;
     if (wave == 0) {
-        if (p.mean) p.mean[m] = mean + rest;
+        if (p.mean) p.mean[m] = both_steps(mean, rest);
         if (p.rstd) p.rstd[m] = rstd;
     }
     for (int n = wave; n < p.N; n += 16) {

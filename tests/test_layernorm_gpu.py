@@ -359,3 +359,17 @@ def test_rows_of_a_default_output_start_lines():
         assert yt.shape == (96, M) and yt.stride(1) == 1 and yt.stride(0) == -(-M // 64) * 64 and yt.data_ptr() % 128 == 0
         other, _ = make(96, M, torch.float16)
         assert torch.equal(tw.tw_layernorm_t(xt, Yt=other), yt)
+
+
+@pytest.mark.parametrize("aligned", [True, False])
+@pytest.mark.parametrize("N", [64, 1000, 2500])
+def test_statistics_of_rows_that_are_not_finite(N, aligned):
+    """The mean of a row with an infinity is that infinity, of one with both or with NaN it is NaN; its deviation is NaN."""
+    for t in TYPES.values():
+        x = torch.randn((6, N), device="cuda").to(t)
+        x[0, 3], x[1, N - 1], x[2, 5] = float("inf"), float("-inf"), float("nan")
+        x[3, 1], x[3, 2] = float("inf"), float("-inf")
+        want = x.double().mean(1)
+        for y, mean, rstd, c in both_boundaries(x, None, None, aligned):
+            assert bool(((mean[:2] == want[:2].float()) & torch.isinf(mean[:2])).all()) and bool(torch.isnan(mean[2:4]).all())
+            assert bool(torch.isnan(rstd[:4]).all()) and bool(torch.isfinite(rstd[4:]).all()) and bool(torch.isfinite(mean[4:]).all())
