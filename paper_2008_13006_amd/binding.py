@@ -254,19 +254,28 @@ def _launch_stream(like, stream) -> int:
     """The raw handle of `stream` (None: the current one) for a call whose operands lie beside `like`: the library launches on the current device,
     so they and the stream have to be of it."""
     device = _current_device()
-    assert like.get_device() == device and (stream is None or stream.device_index == device), "operands and stream have to be of the current device"
+    assert like.get_device() == device and (stream is None or getattr(stream, "device_index", device) == device), "operands and stream have to be of the current device"
     return _raw_stream(device) if stream is None else stream.cuda_stream
+
+
+def _on(stream):
+    """The context in which `stream` (None: the current one) is current.  Any object with a `cuda_stream`, a raw handle, stands for a stream."""
+    if stream is None:
+        return contextlib.nullcontext()
+    cuda = _torch().cuda
+    return cuda.stream(stream if isinstance(stream, cuda.Stream) else cuda.ExternalStream(stream.cuda_stream))
 
 
 def _empty(shape, like, stream, dtype=None):
     """Uninitialised memory that a call allocates beside `like`: an output or scratch.  It is allocated on the stream that uses it, so
     that it comes from that stream's pool, where nothing of the current stream's is still at work, and goes back there.  (Another stream that
-    is to read an output has to wait for this one, as for any result.)"""
+    is to read an output has to wait for this one, and record_stream what it may still read when the tensor is dropped, as for any
+    result.)"""
     torch = _torch()
     dtype = like.dtype if dtype is None else dtype
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=like.device)
-    with torch.cuda.stream(stream):
+    with _on(stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
@@ -338,7 +347,7 @@ class TwWeight:
         if need > self.workspace.numel():
             torch = _torch()
             self._retired.append(self.workspace)
-            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            with _on(stream):
                 self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.workspace.device)
         return self.workspace.data_ptr(), need
 

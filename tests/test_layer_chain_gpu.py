@@ -207,3 +207,26 @@ def test_what_a_call_allocates_belongs_to_its_stream(tw, name):
         assert stream_of(x) == side.cuda_stream and torch.equal(x, y)
     assert fresh.workspace is held or stream_of(fresh.workspace) == side.cuda_stream
     side.synchronize()
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_raw_handles_stand_for_streams(tw, name):
+    """Whatever has a `cuda_stream`: outputs that are not given come from that stream's memory as well."""
+    class Handle:
+        def __init__(self, stream):
+            self.cuda_stream = stream.cuda_stream
+
+    t, M, K, N = torch.float16, 64, 512, 256
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    w = W.generate(W.small_spec("handles", M=1, K=K, N=N, G=64, dtype="f16", col_prune=0.05, keep=("upow", 0.1, 0.5), seed_offset=9450))
+    weight = tw.TwWeight(tw.tw_pack(w.B, w.mask, 64, "f16"))
+    o = {k: torch.randn(s, generator=gen, device="cuda").to(t) for k, s in (("a", (M, K)), ("r", (M, N)), ("b", (K, N)))}
+    o.update(at=o["a"].t().contiguous(), rt=o["r"].t().contiguous(), mean=torch.zeros(M, device="cuda"), rstd=torch.ones(M, device="cuda"))
+    want = CALLS[name](tw, o, weight, None)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = CALLS[name](tw, o, weight, Handle(side))
+    torch.cuda.current_stream().wait_stream(side)
+    for x, y in zip(got, want) if isinstance(got, tuple) else [(got, want)]:
+        assert torch.equal(x, y)
+    side.synchronize()
